@@ -47,6 +47,8 @@ typedef enum {
   RF_ERR_CUDA = 4,
   RF_ERR_TIMEOUT = 5,
   RF_ERR_STATIC_SCRATCH_TOO_SMALL = 6,
+  RF_ERR_CACHE_FULL = 8,   /* the page pool or a row of the page table has no room for the tokens (through dev_status) */
+  RF_ERR_NOT_FINITE = 9,   /* NaN or infinite values went into the cache (through dev_status; see rf_cache_append) */
   RF_ERR_BOUNDS = 7   /* only from a library built with -DRF_BOUNDS_CHECK: a kernel was about to index outside an
                          array (reported through dev_status; the access is skipped, nothing traps) */
 } rf_status;
@@ -335,6 +337,123 @@ void rf_host_pipeline_destroy(rf_host_pipeline *p);
 #define RF_ARM_STATIC_SCRATCH_FLOATS (1u << 20)
 rf_status rf_arm_classify_noalloc(const rf_shape *shape, const rf_params *params, const void *q, const void *k,
                                   int32_t *head_class, float *recall, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * A paged K/V cache in 8 bits, for clips that are generated chunk by chunk: the finished frames' K and V stay on the device and
+ * the next chunk's queries attend to them.  (The paper attends to a whole clip at once; this is the same attention, Eq. 1-2, for a
+ * clip that grows.  Block selection stands where ARM and the block mask stand for a whole clip.)
+ *
+ * A page holds RF_CACHE_PAGE tokens of one sequence, all K/V heads; a sequence is a row of the page table: its token t lies in
+ * page page_table[t / RF_CACHE_PAGE].  Stored values are e4m3 codes times a power of two, one per page, head and tensor (a block of
+ * RF_CACHE_PAGE tokens): such a product is exactly a bf16 value, so the attention kernels round nothing when they widen it.
+ * Codes 0x7f and 0xff (NaN) are never written and must not be: they are read as +-480.
+ *
+ * Everything below is device memory owned by the caller; the struct itself is host memory, read during the call.  A page is
+ * free when no row names it among its first ceil(seq_len / RF_CACHE_PAGE) entries: there are no reference counts to keep, and
+ * rows may name the same page (after rf_cache_fork).  Whatever lies behind a sequence's last token, in its last page or in its row of
+ * the table, is not read.  All pages may start uninitialised; a new cache has seq_len = 0 everywhere.
+ *
+ * Calls that write to a cache and calls that read it are ordered by the caller (one stream, or events), like any buffer's.
+ * Limits: D in {64, 96, 128}; n_seqs <= 1024; heads * n_seqs <= 65535; n_pages <= 524288; max_pages <= 2^23.
+ * seq_len outside 0..max_pages * RF_CACHE_PAGE or a page number outside 0..n_pages-1 is reported as RF_ERR_INVALID_ARG through
+ * dev_status: calls that write then change nothing, calls that read give arbitrary results for that sequence.
+ */
+#define RF_CACHE_PAGE 128
+typedef struct {
+  int32_t n_seqs, heads, D;        /* sequences (the batch), K/V heads, head dimension */
+  int32_t n_pages, max_pages;      /* pages in the pool; columns of the page table */
+  uint8_t *k, *v;                  /* e4m3 [n_pages, heads, RF_CACHE_PAGE, D], 16-byte aligned */
+  float   *k_scale, *v_scale;      /* [n_pages, heads], powers of two in [2^-100, 2^100] */
+  float   *k_sum;                  /* [n_pages, heads, D]: sum of the page's stored keys when it was last written, 16-byte aligned;
+                                      rf_cache_select scores full pages by it */
+  int32_t *page_table;             /* [n_seqs, max_pages] */
+  int32_t *seq_len;                /* [n_seqs] */
+} rf_cache;
+
+/* Bytes of device workspace that rf_cache_append and rf_cache_compact need, 256-byte aligned; 0 on bad arguments.  Its content
+ * means nothing between calls. */
+size_t rf_cache_workspace_bytes(const rf_cache *cache);
+
+/*
+ * Appends new_len[b] tokens to every sequence b (two launches).
+ *   k, v     device bf16 [n_seqs, heads, M, D], 16-byte aligned; rows from new_len[b] on are not read
+ *   new_len  device int32 [n_seqs], each in 0..M; NULL: M tokens for every sequence
+ * Pages come from the pool, the lowest free ones first, sequence by sequence.  A last page that is not full and that another
+ * entry of the table names too is copied to a page of its own first (copy on write).  Per page, head and tensor: the scale is
+ * 2^e with the least e in -100..100 for which no new finite value exceeds 448 * 2^e, or the old scale where the page keeps
+ * tokens and that is larger; codes are the values divided by it, rounded to nearest even, saturating.  (A scale that grows
+ * under old tokens moves their codes by a power of two: only values below the smallest normal code are rounded again.)
+ * Infinities are stored as the largest code of their sign, NaN as zero, and both are reported as RF_ERR_NOT_FINITE.
+ * If the pool or a row of the table has no room, RF_ERR_CACHE_FULL is reported and the cache is left as it was.
+ */
+rf_status rf_cache_append(const rf_cache *cache, const void *k, const void *v, int32_t M, const int32_t *new_len, void *ws,
+                          size_t ws_bytes, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Every sequence b becomes what sequence parent[b] is: rows of the page table are copied, pages are shared (and copied by the
+ * append that first writes to one).  parent[b] = b leaves b as it is, -1 empties it; a parent may have any number of children.
+ *   parent   device int32 [n_seqs]; if one is outside -1..n_seqs-1, RF_ERR_INVALID_ARG is reported and nothing changes
+ */
+rf_status rf_cache_fork(const rf_cache *cache, const int32_t *parent, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Takes tokens out of every sequence b: first those from max_len[b] on, then the whole pages [first[b], first[b] + count[b])
+ * of what is left (a sliding window drops its oldest frames' pages; the tokens behind them move up).  Pages that no row
+ * names any longer are free.
+ *   max_len       device int32 [n_seqs] or NULL (nothing is cut off the end)
+ *   first, count  device int32 [n_seqs], or both NULL
+ * A negative entry is reported as RF_ERR_INVALID_ARG and nothing changes; what reaches past the end means up to the end.
+ */
+rf_status rf_cache_drop(const rf_cache *cache, const int32_t *first, const int32_t *count, const int32_t *max_len,
+                        int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Moves pages so that those in use are pages 0 .. n_live-1: the ones behind that, in ascending order, to the free places before
+ * it, in ascending order (two launches).  The table follows; shared pages stay shared.
+ *   n_live   device int32, written: pages in use (-1 if the table is broken; nothing is moved then)
+ */
+rf_status rf_cache_compact(const rf_cache *cache, int32_t *n_live, void *ws, size_t ws_bytes, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Queries of a call on the cache.  q is bf16 [n_seqs, H, M, D]; H is a multiple of cache->heads, and heads g * H / heads .. of q
+ * share K/V head g.  Sequence b has q_len[b] <= M query rows: the last q_len[b] tokens of the sequence (which are in the cache already),
+ * row i at position p = seq_len[b] - q_len[b] + i.  Rows from q_len[b] on are padding: not read, and their outputs are not written.
+ * With causal_block = c > 0 a row sees the keys of its own block of c positions and of the blocks before: positions below
+ * (p / c + 1) * c (c = tokens of a frame: frame by frame; 1: token by token), none if p < 0.  c = 0: every key.
+ * The rows of a K/V head, [H / heads * M] one query head after the other, are cut into tiles of RF_CACHE_PAGE rows; a
+ * schedule lists pages (entry c = tokens c * RF_CACHE_PAGE ..) per tile.
+ */
+typedef struct {
+  int32_t H, M;              /* query heads; rows of q per head */
+  int32_t causal_block;      /* >= 0 */
+  float   scale;             /* of q k^T before the softmax; 0: 1 / sqrt(D) */
+} rf_cache_query;
+
+/*
+ * Selects pages for every tile of query rows by a cheap score: the sum of the tile's query rows times the mean of the sequence's
+ * stored keys in the page (in 64 bits, so that the choice does not depend on the order of summation).  Of the pages in which some row of the
+ * tile sees a key, the first keep_first and the last keep_last are listed always, and of the others the top_k of highest score
+ * (of equal ones the lower page; NaN is lowest).
+ *   out   count [n_seqs, heads, nQ] and kv_tile [n_seqs, heads, nQ, nKmax] are written (ascending; entries behind the count are
+ *         left as they were); nQ = ceil(H / heads * M / RF_CACHE_PAGE), nKmax >= min(max_pages, keep_first + keep_last + top_k).
+ *         bitmap and kv_len are not used.  max_pages <= 16384 here (RF_ERR_UNSUPPORTED).
+ */
+rf_status rf_cache_select(const rf_cache *cache, const rf_cache_query *query, const void *q, const int32_t *q_len, int32_t keep_first,
+                          int32_t keep_last, int32_t top_k, rf_schedule *out, int32_t *dev_status, void *cuda_stream);
+
+/*
+ * Attention over the cache (Eq. 1-2 on the sequence's tokens), all pages or those that a schedule lists.
+ *   q       device bf16 [n_seqs, H, M, D], 16-byte aligned; q_len device int32 [n_seqs] in 0..M or NULL (M rows everywhere)
+ *   sched   NULL, or count / kv_tile as rf_cache_select writes them, or the caller's own (ascending, each page once; a page past
+ *           the sequence is reported as RF_ERR_INVALID_ARG and skipped)
+ *   o       device bf16 [n_seqs, H, M, D], 16-byte aligned;  lse  device float [n_seqs, H, M] or NULL (natural log)
+ *           A row that sees no key gets zeros and -inf.
+ *   ws      rf_cache_attn_workspace_bytes() of device memory, 256-byte aligned, overwritten; calls that may overlap need one each
+ */
+size_t rf_cache_attn_workspace_bytes(const rf_cache *cache, const rf_cache_query *query);
+rf_status rf_cache_attn_fwd(const rf_cache *cache, const rf_cache_query *query, const void *q, const int32_t *q_len,
+                            const rf_schedule *sched, void *o, float *lse, void *ws, size_t ws_bytes, int32_t *dev_status,
+                            void *cuda_stream);
 
 #ifdef __cplusplus
 }

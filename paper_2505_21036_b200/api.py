@@ -24,7 +24,10 @@ EXPORTS = ["rf_status_string", "rf_schedule_dims", "rf_workspace_bytes", "rf_arm
            "rf_arm_classify_noalloc", "rf_selftest_wait_timeout", "rf_arm_classify_plus", "rf_build_block_mask_plus", "rf_sparse_attn_fwd_plus",
            "rf_sparse_attn_reordered", "rf_selftest_arm_abandoned", "rf_selftest_sparse_call_abandoned", "rf_bounds_checked", "rf_host_pipeline_staging_bytes",
            "rf_host_pipeline_create", "rf_host_pipeline_run", "rf_host_pipeline_status", "rf_host_pipeline_destroy",
-           "rf_host_pipeline_set_bandwidths", "rf_host_pipeline_head_class", "rf_host_pipeline_head_window"]
+           "rf_host_pipeline_set_bandwidths", "rf_host_pipeline_head_class", "rf_host_pipeline_head_window",
+           "rf_cache_workspace_bytes", "rf_cache_append", "rf_cache_fork", "rf_cache_drop", "rf_cache_compact", "rf_cache_select",
+           "rf_cache_attn_workspace_bytes", "rf_cache_attn_fwd"]
+CACHE_PAGE = 128
 
 
 class rf_shape(C.Structure):
@@ -42,6 +45,15 @@ class rf_params(C.Structure):
 class rf_schedule(C.Structure):
     _fields_ = [("count", C.c_void_p), ("kv_tile", C.c_void_p), ("bitmap", C.c_void_p), ("kv_len", C.c_void_p),
                 ("nQ", C.c_int32), ("nKmax", C.c_int32)]
+
+
+class rf_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "heads", "D", "n_pages", "max_pages")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "k_sum", "page_table", "seq_len")]
+
+
+class rf_cache_query(C.Structure):
+    _fields_ = [("H", C.c_int32), ("M", C.c_int32), ("causal_block", C.c_int32), ("scale", C.c_float)]
 
 
 class RainFusionError(RuntimeError):
@@ -117,6 +129,22 @@ def load():
     lib.rf_dense_attn_fwd.argtypes = [P(rf_shape), V, V, V, V, V, V, Z, V, V]
     lib.rf_dense_attn_fwd_split.restype = I
     lib.rf_dense_attn_fwd_split.argtypes = lib.rf_dense_attn_fwd.argtypes
+    lib.rf_cache_workspace_bytes.restype = Z
+    lib.rf_cache_workspace_bytes.argtypes = [P(rf_cache)]
+    lib.rf_cache_append.restype = I
+    lib.rf_cache_append.argtypes = [P(rf_cache), V, V, C.c_int32, V, V, Z, V, V]
+    lib.rf_cache_fork.restype = I
+    lib.rf_cache_fork.argtypes = [P(rf_cache), V, V, V]
+    lib.rf_cache_drop.restype = I
+    lib.rf_cache_drop.argtypes = [P(rf_cache), V, V, V, V, V]
+    lib.rf_cache_compact.restype = I
+    lib.rf_cache_compact.argtypes = [P(rf_cache), V, V, Z, V, V]
+    lib.rf_cache_select.restype = I
+    lib.rf_cache_select.argtypes = [P(rf_cache), P(rf_cache_query), V, V, C.c_int32, C.c_int32, C.c_int32, P(rf_schedule), V, V]
+    lib.rf_cache_attn_workspace_bytes.restype = Z
+    lib.rf_cache_attn_workspace_bytes.argtypes = [P(rf_cache), P(rf_cache_query)]
+    lib.rf_cache_attn_fwd.restype = I
+    lib.rf_cache_attn_fwd.argtypes = [P(rf_cache), P(rf_cache_query), V, V, P(rf_schedule), V, V, V, Z, V, V]
     _lib = lib
     return lib
 
@@ -362,3 +390,150 @@ def rf_dense_attn_fwd(shape, q, k, v, o, lse, dev_status=None, scratch=None):
     _check(lib.rf_dense_attn_fwd_split(C.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse),
                                        _ptr(scratch), 0 if scratch is None else scratch.numel(), _ptr(dev_status), _stream()),
            "rf_dense_attn_fwd")
+
+
+# ---------------------------------------------------------------------------------------------- the paged 8-bit K/V cache
+def _cache_arg(name, t, dtype, shape, device):
+    """The caller's tensor, checked: the kernels index it as a contiguous array of this type and shape."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise RainFusionError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is wanted, got {t.dtype} {tuple(t.shape)} "
+                              f"{'' if t.is_contiguous() else 'not contiguous '}on {t.device}")
+    return t.data_ptr()
+
+
+class KVCache:
+    """rf_cache over the caller's tensors: k, v float8_e4m3fn (or their bytes as uint8) [n_pages, heads, 128, D]; k_scale, v_scale float
+    [n_pages, heads]; k_sum float [n_pages, heads, D]; page_table int32 [n_seqs, max_pages]; seq_len int32 [n_seqs].  KVCache.empty
+    allocates them.  Holds the workspace of the calls that write to the cache, which are ordered by the caller anyway."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_sum, page_table, seq_len):
+        import torch
+        if k.dim() != 4 or page_table.dim() != 2 or k.shape[2] != CACHE_PAGE or k.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise RainFusionError(f"k: float8_e4m3fn [n_pages, heads, {CACHE_PAGE}, D] is wanted, got {k.dtype} {tuple(k.shape)}")
+        n_pages, heads, _, D = k.shape
+        n_seqs, max_pages = page_table.shape
+        dev = k.device
+        self.c = rf_cache(n_seqs, heads, D, n_pages, max_pages, _cache_arg("k", k, k.dtype, k.shape, dev),
+                          _cache_arg("v", v, k.dtype, k.shape, dev), _cache_arg("k_scale", k_scale, torch.float32, (n_pages, heads), dev),
+                          _cache_arg("v_scale", v_scale, torch.float32, (n_pages, heads), dev),
+                          _cache_arg("k_sum", k_sum, torch.float32, (n_pages, heads, D), dev),
+                          _cache_arg("page_table", page_table, torch.int32, (n_seqs, max_pages), dev),
+                          _cache_arg("seq_len", seq_len, torch.int32, (n_seqs,), dev))
+        self.k, self.v, self.k_scale, self.v_scale, self.k_sum = k, v, k_scale, v_scale, k_sum
+        self.page_table, self.seq_len, self.device = page_table, seq_len, dev
+        self.n_seqs, self.heads, self.D, self.n_pages, self.max_pages = n_seqs, heads, D, n_pages, max_pages
+        self.ref = C.byref(self.c)
+        n = load().rf_cache_workspace_bytes(self.ref)
+        if n == 0:
+            raise RainFusionError("rf_cache_workspace_bytes: unsupported sizes or misaligned tensors")
+        self.ws = torch.empty(n, dtype=torch.uint8, device=dev)
+
+    @classmethod
+    def empty(cls, n_seqs, heads, D, n_pages, max_pages, device):
+        import torch
+        k = torch.empty((n_pages, heads, CACHE_PAGE, D), dtype=torch.float8_e4m3fn, device=device)
+        f = dict(dtype=torch.float32, device=device)
+        i = dict(dtype=torch.int32, device=device)
+        return cls(k, torch.empty_like(k), torch.empty((n_pages, heads), **f), torch.empty((n_pages, heads), **f),
+                   torch.empty((n_pages, heads, D), **f), torch.zeros((n_seqs, max_pages), **i), torch.zeros((n_seqs,), **i))
+
+    def ints(self, name, t, n=None):
+        """A device int32 argument [n_seqs] (or [n]); None stays None."""
+        import torch
+        return _cache_arg(name, t, torch.int32, (self.n_seqs if n is None else n,), self.device)
+
+    def stream(self):
+        """The current stream, which has to be the cache's device's."""
+        import torch
+        if self.device.index != torch.cuda.current_device():
+            raise RainFusionError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
+        return _stream()
+
+
+class CacheSchedule:
+    """Lists of pages for the tiles of query rows of a call: count int32 [n_seqs, heads, nQ], pages int32 [n_seqs, heads, nQ, capacity]."""
+
+    def __init__(self, count, pages):
+        import torch
+        if pages.dim() != 4:
+            raise RainFusionError("pages: [n_seqs, heads, nQ, capacity] is wanted")
+        self.count, self.pages = count, pages
+        self.c = rf_schedule(_cache_arg("count", count, torch.int32, pages.shape[:3], pages.device),
+                             _cache_arg("pages", pages, torch.int32, pages.shape, pages.device), None, None, pages.shape[2], pages.shape[3])
+        self.ref = C.byref(self.c)
+
+    @classmethod
+    def empty(cls, cache: KVCache, H: int, M: int, capacity: int):
+        import torch
+        n_q = -(-(H // cache.heads) * M // CACHE_PAGE)
+        i = dict(dtype=torch.int32, device=cache.device)
+        return cls(torch.zeros((cache.n_seqs, cache.heads, n_q), **i), torch.zeros((cache.n_seqs, cache.heads, n_q, capacity), **i))
+
+
+def alloc_cache_attn_workspace(cache: KVCache, H: int, M: int):
+    import torch
+    query = rf_cache_query(H, M, 0, 0.0)
+    n = load().rf_cache_attn_workspace_bytes(cache.ref, C.byref(query))
+    if n == 0:
+        raise RainFusionError("rf_cache_attn_workspace_bytes: invalid or unsupported sizes")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def rf_cache_append(cache: KVCache, k, v, new_len=None, dev_status=None):
+    """k, v: bf16 [n_seqs, heads, M, D]; new_len: int32 [n_seqs] on the device, or None for M tokens everywhere."""
+    import torch
+    shape = (cache.n_seqs, cache.heads, k.shape[2] if k.dim() == 4 else -1, cache.D)
+    _check(load().rf_cache_append(cache.ref, _cache_arg("k", k, torch.bfloat16, shape, cache.device),
+                                  _cache_arg("v", v, torch.bfloat16, shape, cache.device), shape[2], cache.ints("new_len", new_len),
+                                  cache.ws.data_ptr(), cache.ws.numel(), cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_append")
+
+
+def rf_cache_fork(cache: KVCache, parent, dev_status=None):
+    _check(load().rf_cache_fork(cache.ref, cache.ints("parent", parent), cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_fork")
+
+
+def rf_cache_drop(cache: KVCache, first=None, count=None, max_len=None, dev_status=None):
+    _check(load().rf_cache_drop(cache.ref, cache.ints("first", first), cache.ints("count", count), cache.ints("max_len", max_len),
+                                cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_drop")
+
+
+def rf_cache_compact(cache: KVCache, n_live, dev_status=None):
+    _check(load().rf_cache_compact(cache.ref, cache.ints("n_live", n_live, 1), cache.ws.data_ptr(), cache.ws.numel(),
+                                   cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_compact")
+
+
+def _cache_query(cache, q, causal_block, scale):
+    import torch
+    if q.dim() != 4:
+        raise RainFusionError("q: [n_seqs, H, M, D] is wanted")
+    return (_cache_arg("q", q, torch.bfloat16, (cache.n_seqs, q.shape[1], q.shape[2], cache.D), cache.device),
+            rf_cache_query(q.shape[1], q.shape[2], causal_block, 0.0 if scale is None else scale))
+
+
+def rf_cache_select(cache: KVCache, q, sched: CacheSchedule, q_len=None, causal_block=0, keep_first=0, keep_last=0, top_k=0, dev_status=None):
+    """Fills sched with the pages that the tiles of query rows of q [n_seqs, H, M, D] attend to."""
+    ptr, query = _cache_query(cache, q, causal_block, None)
+    if tuple(sched.pages.shape[:2]) != (cache.n_seqs, cache.heads) or sched.pages.device != cache.device:
+        raise RainFusionError("the schedule was not made for this cache")
+    _check(load().rf_cache_select(cache.ref, C.byref(query), ptr, cache.ints("q_len", q_len), keep_first, keep_last, top_k, sched.ref,
+                                  cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_select")
+
+
+def rf_cache_attn_fwd(cache: KVCache, q, o, lse=None, sched: Optional[CacheSchedule] = None, q_len=None, causal_block=0, scale=None, ws=None,
+                      dev_status=None):
+    """q, o: bf16 [n_seqs, H, M, D]; lse: float [n_seqs, H, M] or None; ws: alloc_cache_attn_workspace(cache, H, M), by default a block
+    from torch's allocator for the time of the call."""
+    import torch
+    ptr, query = _cache_query(cache, q, causal_block, scale)
+    if ws is None:
+        ws = alloc_cache_attn_workspace(cache, q.shape[1], q.shape[2])
+    if ws.device != cache.device:
+        raise RainFusionError("ws is not on the cache's device")
+    if sched is not None and (tuple(sched.pages.shape[:2]) != (cache.n_seqs, cache.heads) or sched.pages.device != cache.device):
+        raise RainFusionError("the schedule was not made for this cache")
+    _check(load().rf_cache_attn_fwd(cache.ref, C.byref(query), ptr, cache.ints("q_len", q_len), None if sched is None else sched.ref,
+                                    _cache_arg("o", o, torch.bfloat16, q.shape, cache.device),
+                                    _cache_arg("lse", lse, torch.float32, q.shape[:3], cache.device), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                    cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_attn_fwd")

@@ -3,6 +3,7 @@
 #include <math.h>
 #include <string.h>
 
+#include "rf_cache.cuh"
 #include "rf_common.cuh"
 
 namespace {
@@ -153,6 +154,18 @@ bool rf_encode_rows_map(CUtensorMap* m, const void* ptr, int D, int rows, size_t
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, box_columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool rf_encode_pages_map(CUtensorMap* m, const uint8_t* codes, const RfCache& c) {
+  EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)c.D, (cuuint64_t)kPage, (cuuint64_t)c.n_pages * c.H};
+  cuuint64_t strides[2] = {(cuuint64_t)c.D, (cuuint64_t)kPage * c.D};
+  cuuint32_t box[3] = {c.D == 64 ? 64u : 128u, (cuuint32_t)kPage, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            c.D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -397,6 +410,8 @@ const char* rf_status_string(rf_status s) {
     case RF_ERR_TIMEOUT: return "device-side wait timed out";
     case RF_ERR_STATIC_SCRATCH_TOO_SMALL:
       return "problem needs more scratch than the library's built-in array holds (use the workspace entry point)";
+    case RF_ERR_CACHE_FULL: return "no room left in the cache (pages of the pool or columns of the page table)";
+    case RF_ERR_NOT_FINITE: return "NaN or infinite values went into the cache";
     case RF_ERR_BOUNDS: return "a kernel of the bounds-checking build was about to index outside an array";
   }
   return "unknown status";

@@ -1,0 +1,721 @@
+// The paged 8-bit K/V cache: appending, page operations, selection of pages.
+//
+// All of its state is on the device and every call is a fixed sequence of launches, so whole steps can be captured.  Which
+// pages are free follows from the page table alone (those that no row names), so there are no reference counts that could
+// disagree with it: a planning kernel of one CTA marks the named pages in a bitmap in shared memory, where a second
+// bitmap tells the pages that are named more than once.
+#include <math.h>
+
+#include "rf_cache.cuh"
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive prefix sum over the CTA's kPlanThreads values; `total` for everybody.  s: 33 ints of shared memory.
+__device__ __forceinline__ int block_scan(int v, int* s, int& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();                       // the last scan's sums have been read
+  if (lane == 31) s[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int t = s[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, t, d);
+      if (lane >= d) t += y;
+    }
+    s[lane] = t;
+  }
+  __syncthreads();
+  total = s[31];
+  return x - v + (warp ? s[warp - 1] : 0);
+}
+
+// Workspace words: per sequence {old length, new tokens, page that held its partly filled last page}, a few counts, then
+// two lists of n_pages words.
+enum { kWsCount = 0, kWsHead = 64 };
+struct PlanWs {
+  int32_t *count, *old_len, *n_new, *src, *list, *to;
+};
+__host__ __device__ __forceinline__ PlanWs plan_ws(int32_t* ws, int B, int n_pages) {
+  PlanWs w;
+  w.count = ws + kWsCount;
+  w.old_len = ws + kWsHead;
+  w.n_new = w.old_len + B;
+  w.src = w.n_new + B;
+  w.list = w.src + B;
+  w.to = w.list + n_pages;
+  return w;
+}
+
+// Marks the pages that the table names; `lens` in shared memory, all in range; *most_pages (shared memory too) becomes the
+// longest row's number of pages.  False for everybody if an entry is none.
+__device__ __forceinline__ bool mark_pages(const RfCache& c, const int* lens, uint32_t* used, uint32_t* twice, int words, int* most_pages) {
+  for (int i = threadIdx.x; i < words; i += kPlanThreads) {
+    used[i] = 0u;
+    if (twice != nullptr) twice[i] = 0u;
+  }
+  if (threadIdx.x == 0) *most_pages = 0;
+  __syncthreads();
+  if (threadIdx.x < c.B) atomicMax(most_pages, rf_pages(lens[threadIdx.x]));
+  __syncthreads();
+  bool bad = false;
+  const int most = *most_pages;
+  // Over the rows' used columns only.  (The products fit: n_seqs * max_pages < 2^33, in 64 bits.)
+  const long long n = (long long)c.B * most;
+  for (long long i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int b = (int)(i / most), col = (int)(i - (long long)b * most);
+    if (col >= rf_pages(lens[b])) continue;
+    const int p = c.table[(size_t)b * c.max_pages + col];
+    if (p < 0 || p >= c.n_pages) {
+      bad = true;
+      continue;
+    }
+    const uint32_t bit = 1u << (p & 31), before = atomicOr(&used[p >> 5], bit);
+    if (twice != nullptr && (before & bit)) atomicOr(&twice[p >> 5], bit);
+  }
+  return !__syncthreads_or(bad);
+}
+
+// ------------------------------------------------------------------------------------------------ append
+// Pages for the tokens that come, and the sequences' new lengths.  One CTA: what it does is a chain of a dozen round trips
+// to the L2, 5 to 7 us, whatever the pool's size up to some ten thousand pages.
+__global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, int M, const int32_t* new_len, int32_t* ws, int32_t* dev_status) {
+  extern __shared__ uint32_t bits[];
+  __shared__ int scan[33], lens[kCacheMaxSeqs], need_at[kCacheMaxSeqs + 1], most;
+  const int tid = threadIdx.x, words = (c.n_pages + 31) / 32;
+  uint32_t *used = bits, *twice = bits + words;
+  const PlanWs w = plan_ws(ws, c.B, c.n_pages);
+  rf_grid_trigger();
+  rf_grid_wait();
+
+  int len = 0, add = 0;
+  bool bad = false, full = false;
+  if (tid < c.B) {
+    len = c.len[tid];
+    add = new_len != nullptr ? new_len[tid] : M;
+    const long long most = (long long)c.max_pages * kPage;
+    bad = len < 0 || len > most || add < 0 || add > M;
+    full = !bad && (long long)len + add > min(most, 0x7fffffffll);
+    lens[tid] = bad ? 0 : len;
+  }
+  bad = __syncthreads_or(bad);
+  if (!bad) bad = !mark_pages(c, lens, used, twice, words, &most);
+  // fresh pages of this thread's sequence; its partly filled last page is among them if others name it too
+  int need = 0, first_new = 0, shared_page = 0, old_page = -1;
+  if (!bad && tid < c.B && add > 0 && !full) {
+    first_new = rf_pages(len);
+    need = rf_pages(len + add) - first_new;
+    if (len % kPage != 0) {
+      old_page = c.table[(size_t)tid * c.max_pages + len / kPage];
+      shared_page = (twice[old_page >> 5] >> (old_page & 31)) & 1u;
+      need += shared_page;
+    }
+  }
+  int total, n_free, at = block_scan(need, scan, total);
+  const int per = (words + kPlanThreads - 1) / kPlanThreads, w0 = min(tid * per, words), w1 = min(w0 + per, words);
+  auto free_of = [&](int i) -> uint32_t {
+    const uint32_t f = ~used[i];
+    return i == words - 1 && (c.n_pages & 31) ? f & ((1u << (c.n_pages & 31)) - 1u) : f;
+  };
+  int mine = 0;
+  for (int i = w0; i < w1; ++i) mine += __popc(free_of(i));
+  int rank = block_scan(mine, scan, n_free);
+  full = __syncthreads_or(full) || total > n_free;
+  if (bad || full) {
+    if (tid == 0) rf_report(dev_status, bad ? RF_ERR_INVALID_ARG : RF_ERR_CACHE_FULL);
+    if (tid < c.B) w.n_new[tid] = 0;
+    return;
+  }
+  if (tid < c.B) need_at[tid] = at;
+  if (tid == 0) need_at[c.B] = total;
+  for (int i = w0; i < w1 && rank < total; ++i)
+    for (uint32_t f = free_of(i); f != 0u && rank < total; f &= f - 1u) w.list[rank++] = i * 32 + __ffs(f) - 1;
+  if (tid < c.B) {
+    w.old_len[tid] = len;
+    w.n_new[tid] = add;
+    w.src[tid] = old_page;
+    c.len[tid] = len + add;
+    lens[tid] = first_new - shared_page;       // the first column that gets a fresh page
+  }
+  __syncthreads();
+  for (int i = tid; i < total; i += kPlanThreads) {
+    int lo = 0, hi = c.B - 1;                   // the last sequence whose pages begin at i or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (need_at[mid] <= i) lo = mid; else hi = mid - 1;
+    }
+    const int col = lens[lo] + i - need_at[lo];
+    if (rf_in_bounds(col, c.max_pages, dev_status)) c.table[(size_t)lo * c.max_pages + col] = w.list[i];
+  }
+}
+
+// e4m3 code -> its value in units of 2^-9 (an integer of at most 18 bits and a sign).
+__device__ __forceinline__ int code_units(uint32_t code) {
+  const int e = (code >> 3) & 15, m = code & 7;
+  const int v = e == 0 ? m : (8 + m) << (e - 1);
+  return code & 0x80 ? -v : v;
+}
+__device__ __forceinline__ float code_value(uint32_t code) { return (float)code_units(code) * 0.001953125f; }
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
+// One page of one head, K or V.  A thread takes 8 columns (16 bytes in, 8 out) of every 16th row, all loads first; the page's
+// largest magnitude has to be known before the first code, so a page is held in registers and read once.  Bound by HBM for
+// whole frames (6 bytes a pair of values of K and V); for single tokens by the two launches.  The page's old tokens are
+// read and written again only where they move to another page or another scale; K's are read for the sum.
+// The sum of the codes is taken in integers, so it is the same however the page was filled.
+template <int D>
+__global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const __nv_bfloat16* kx, const __nv_bfloat16* vx, int M, const int32_t* ws,
+                                                               int32_t* dev_status) {
+  constexpr int kCols = D / 8, kPasses = kPage / 16, kThreads = 2 * D;
+  static_assert(kCols * 16 == kThreads, "a pass is 16 rows");
+  __shared__ int red[kThreads / 32], sums[D];
+  const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z >> 1, col = tid % kCols, row0 = tid / kCols;
+  const bool keys = (blockIdx.z & 1) == 0;
+  const PlanWs w = plan_ws(const_cast<int32_t*>(ws), c.B, c.n_pages);
+  rf_grid_trigger();
+  rf_grid_wait();
+  const int add = w.n_new[b];
+  if (add == 0) return;
+  const int len = w.old_len[b], page = len / kPage + blockIdx.x, t0 = page * kPage;
+  if (t0 >= len + add) return;
+  const int held = max(0, min(kPage, len - t0)), end = min(kPage, len + add - t0);
+  const int dst = c.table[(size_t)b * c.max_pages + page];
+  if (!rf_in_bounds(dst, c.n_pages, dev_status)) return;
+  const int src = held ? w.src[b] : dst;
+  if (tid < D) sums[tid] = 0;
+
+  const __nv_bfloat16* x = (keys ? kx : vx) + (((size_t)b * c.H + h) * M + (t0 - len)) * D + col * 8;
+  const size_t block = (size_t)kPage * D;
+  uint8_t* data = keys ? c.k : c.v;
+  const uint8_t* old = data + ((size_t)src * c.H + h) * block + col * 8;
+  uint8_t* out = data + ((size_t)dst * c.H + h) * block + col * 8;
+  float* scales = keys ? c.k_scale : c.v_scale;
+  const uint32_t old_bits = held ? __float_as_uint(scales[(size_t)src * c.H + h]) : 0u;
+  uint4 v[kPasses];
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) {
+    const int r = row0 + 16 * p;
+    v[p] = make_uint4(0u, 0u, 0u, 0u);
+    if (r < held) {
+      const uint2 t = *reinterpret_cast<const uint2*>(old + (size_t)r * D);
+      v[p].x = t.x; v[p].y = t.y;
+    } else if (r < end) {
+      v[p] = *reinterpret_cast<const uint4*>(x + (size_t)r * D);
+    }
+  }
+  // largest finite magnitude of the new tokens, as bf16 bits
+  uint32_t most = 0u;
+  bool odd = false;
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) {
+    const int r = row0 + 16 * p;
+    if (r < held || r >= end) continue;
+    const uint32_t* u = &v[p].x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
+      const bool flo = lo < 0x7f80u, fhi = hi < 0x7f80u;
+      odd |= !flo | !fhi;
+      most = max(most, max(flo ? lo : 0u, fhi ? hi : 0u));
+    }
+  }
+  if (odd) rf_report(dev_status, RF_ERR_NOT_FINITE);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((tid & 31) == 0) red[tid >> 5] = (int)most;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) most = max(most, (uint32_t)red[i]);
+  // 448 = 1.75 * 2^8, so with m * 2^E the largest magnitude e is E - 8, or E - 7 where m > 1.75; subnormal ones end at -100
+  int e = (int)(most >> 7) - 127 - ((most & 127u) > 96u ? 7 : 8);
+  e = min(max(e, -100), 100);
+  const int e_old = (int)(old_bits >> 23) - 127;
+  const bool moves = held && (src != dst || e > e_old);    // old tokens get another place or scale
+  const int e_new = held ? max(e, min(max(e_old, -100), 100)) : e;
+  const float inv = pow2f(-e_new);
+  const float again = held ? pow2f(max(min(max(e_old, -100), 100) - e_new, -126)) : 1.f;
+  int acc[8] = {};
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) {
+    const int r = row0 + 16 * p;
+    if (r >= end) continue;
+    uint2 code;
+    if (r < held) {
+      code = make_uint2(v[p].x, v[p].y);
+      if (again != 1.f) {
+        uint32_t* cw = &code.x;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t t = cw[i];
+          const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(code_value(t & 255u) * again, code_value((t >> 8) & 255u) * again), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t z = __nv_cvt_float2_to_fp8x2(make_float2(code_value((t >> 16) & 255u) * again, code_value(t >> 24) * again), __NV_SATFINITE, __NV_E4M3);
+          cw[i] = a | (z << 16);
+        }
+      }
+    } else {
+      uint32_t* cw = &code.x;
+      const uint32_t* u = &v[p].x;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t half = j & 1 ? u[2 * i + j / 2] & 0xffff0000u : u[2 * i + j / 2] << 16;
+          f[j] = (half & 0x7fffffffu) > 0x7f800000u ? 0.f : __uint_as_float(half) * inv;   // NaN -> 0; infinities saturate
+        }
+        const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t z = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+        cw[i] = a | (z << 16);
+      }
+    }
+    if (r >= held || moves) *reinterpret_cast<uint2*>(out + (size_t)r * D) = code;
+    if (keys) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        acc[i] += code_units((code.x >> (8 * i)) & 255u);
+        acc[4 + i] += code_units((code.y >> (8 * i)) & 255u);
+      }
+    }
+  }
+  const size_t side = (size_t)dst * c.H + h;
+  if (tid == 0) scales[side] = pow2f(e_new);
+  if (!keys) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) atomicAdd(&sums[col * 8 + i], acc[i]);
+  __syncthreads();
+  if (tid < D) c.k_sum[side * D + tid] = (float)sums[tid] * 0.001953125f * pow2f(e_new);
+}
+
+// ------------------------------------------------------------------------------------------------ fork, drop
+// Thirty-two columns of the table: the old rows are taken into shared memory and written back in their new places.
+__global__ void __launch_bounds__(256) rf_cache_fork_kernel(RfCache c, const int32_t* parent, int32_t* dev_status) {
+  extern __shared__ int rows[];                       // [B][32], then the lengths in CTA 0
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, col = blockIdx.x * 32 + lane;
+  rf_grid_trigger();
+  rf_grid_wait();
+  bool bad = false;
+  for (int b = tid; b < c.B; b += 256) bad |= parent[b] < -1 || parent[b] >= c.B;
+  for (int b = warp; b < c.B; b += 8)
+    if (col < c.max_pages) rows[b * 32 + lane] = c.table[(size_t)b * c.max_pages + col];
+  int* lens = rows + c.B * 32;
+  if (blockIdx.x == 0)
+    for (int b = tid; b < c.B; b += 256) lens[b] = c.len[b];
+  if (__syncthreads_or(bad)) {
+    if (blockIdx.x == 0 && tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
+    return;
+  }
+  for (int b = warp; b < c.B; b += 8) {
+    const int p = parent[b];
+    if (p >= 0 && p != b && col < c.max_pages) c.table[(size_t)b * c.max_pages + col] = rows[p * 32 + lane];
+  }
+  if (blockIdx.x == 0)
+    for (int b = tid; b < c.B; b += 256) c.len[b] = parent[b] < 0 ? 0 : lens[parent[b]];
+}
+
+__global__ void __launch_bounds__(256) rf_cache_drop_kernel(RfCache c, const int32_t* first, const int32_t* count, const int32_t* max_len, int32_t* dev_status) {
+  const int tid = threadIdx.x, b = blockIdx.x;
+  rf_grid_trigger();
+  rf_grid_wait();
+  bool bad = false;
+  for (int i = tid; i < c.B; i += 256) {
+    if (max_len != nullptr) bad |= max_len[i] < 0;
+    if (first != nullptr) bad |= first[i] < 0 || count[i] < 0;
+  }
+  int len = c.len[b];                                  // (read by everybody before the barrier, written after it)
+  if (__syncthreads_or(bad)) {
+    if (b == 0 && tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
+    return;
+  }
+  if (len < 0 || (long long)len > (long long)c.max_pages * kPage) {
+    if (tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
+    return;
+  }
+  if (max_len != nullptr) len = min(len, max_len[b]);
+  const int pages = rf_pages(len);
+  if (first != nullptr) {
+    const int from = min(first[b], pages), n = min(count[b], pages - from);
+    if (n > 0) {
+      int32_t* row = c.table + (size_t)b * c.max_pages;
+      for (int base = from + n; base < pages; base += 256) {      // ascending: a stretch is read before it is written over
+        const int i = base + tid, p = i < pages ? row[i] : 0;
+        __syncthreads();
+        if (i < pages) row[i - n] = p;
+        __syncthreads();
+      }
+      len -= min(len, (from + n) * kPage) - from * kPage;
+    }
+  }
+  if (tid == 0) c.len[b] = len;
+}
+
+// ------------------------------------------------------------------------------------------------ compact
+__global__ void __launch_bounds__(kPlanThreads) rf_cache_compact_plan_kernel(RfCache c, int32_t* n_live, int32_t* ws, int32_t* dev_status) {
+  extern __shared__ uint32_t bits[];
+  __shared__ int scan[33], lens[kCacheMaxSeqs], most;
+  const int tid = threadIdx.x, words = (c.n_pages + 31) / 32;
+  uint32_t* used = bits;
+  const PlanWs w = plan_ws(ws, c.B, c.n_pages);
+  rf_grid_trigger();
+  rf_grid_wait();
+  bool bad = false;
+  if (tid < c.B) {
+    const int len = c.len[tid];
+    bad = len < 0 || (long long)len > (long long)c.max_pages * kPage;
+    lens[tid] = bad ? 0 : len;
+  }
+  bad = __syncthreads_or(bad);
+  if (!bad) bad = !mark_pages(c, lens, used, nullptr, words, &most);
+  if (bad) {
+    if (tid == 0) {
+      rf_report(dev_status, RF_ERR_INVALID_ARG);
+      *w.count = 0;
+      *n_live = -1;
+    }
+    return;
+  }
+  const int per = (words + kPlanThreads - 1) / kPlanThreads, w0 = min(tid * per, words), w1 = min(w0 + per, words);
+  int mine = 0, live, moves, n;
+  for (int i = w0; i < w1; ++i) mine += __popc(used[i]);
+  block_scan(mine, scan, live);
+  // bits of word i that lie before page `live`
+  auto below = [&](int i) -> uint32_t {
+    const int d = live - i * 32;
+    return d >= 32 ? 0xffffffffu : d <= 0 ? 0u : (1u << d) - 1u;
+  };
+  int holes = 0, movers = 0;
+  for (int i = w0; i < w1; ++i) {
+    holes += __popc(~used[i] & below(i));
+    movers += __popc(used[i] & ~below(i));
+  }
+  int hole_at = block_scan(holes, scan, n), mover_at = block_scan(movers, scan, moves);   // n == moves
+  for (int i = w0; i < w1; ++i)
+    for (uint32_t f = ~used[i] & below(i); f != 0u; f &= f - 1u) w.to[hole_at++] = i * 32 + __ffs(f) - 1;
+  for (int i = w0; i < w1; ++i)
+    for (uint32_t f = used[i] & ~below(i); f != 0u; f &= f - 1u) w.list[mover_at++] = i * 32 + __ffs(f) - 1;
+  if (tid == 0) {
+    *w.count = moves;
+    *n_live = live;
+  }
+  __syncthreads();
+  const long long all = (long long)c.B * most;
+  for (long long i = tid; i < all; i += kPlanThreads) {
+    const int b = (int)(i / most), col = (int)(i - (long long)b * most);
+    if (col >= rf_pages(lens[b])) continue;
+    int32_t* entry = c.table + (size_t)b * c.max_pages + col;
+    const int p = *entry;
+    if (p < live) continue;
+    int lo = 0, hi = moves - 1;                 // its place among the moving pages, which ascend
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (w.list[mid] < p) lo = mid + 1; else hi = mid;
+    }
+    *entry = w.to[lo];
+  }
+}
+
+// Copies page list[i] to page to[i]: a work item is one head of one moving page, K or V, 16 KB at D = 128.  Sources lie
+// behind the live pages' number and destinations before it, so no item reads what another writes.
+__global__ void __launch_bounds__(256) rf_cache_move_kernel(RfCache c, const int32_t* ws, int32_t* dev_status) {
+  rf_grid_trigger();
+  rf_grid_wait();
+  const PlanWs w = plan_ws(const_cast<int32_t*>(ws), c.B, c.n_pages);
+  const int moves = *w.count, tid = threadIdx.x, n16 = kPage * c.D / 16;
+  const long long items = (long long)moves * c.H * 2;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int m = (int)(it / (2 * c.H)), r = (int)(it % (2 * c.H)), h = r >> 1;
+    const bool keys = (r & 1) == 0;
+    const int from = w.list[m], to = w.to[m];
+    if (!rf_in_bounds(from, c.n_pages, dev_status) || !rf_in_bounds(to, c.n_pages, dev_status)) continue;
+    const size_t sf = (size_t)from * c.H + h, st = (size_t)to * c.H + h;
+    uint8_t* data = keys ? c.k : c.v;
+    const uint4* s = reinterpret_cast<const uint4*>(data + sf * kPage * c.D);
+    uint4* d = reinterpret_cast<uint4*>(data + st * kPage * c.D);
+    uint4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (tid + i * 256 < n16) v[i] = s[tid + i * 256];
+    float sum = 0.f;
+    if (keys && tid < c.D) sum = c.k_sum[sf * c.D + tid];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (tid + i * 256 < n16) d[tid + i * 256] = v[i];
+    if (keys && tid < c.D) c.k_sum[st * c.D + tid] = sum;
+    if (tid == 0) {
+      float* scales = keys ? c.k_scale : c.v_scale;
+      scales[st] = scales[sf];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ select
+// One CTA per tile of query rows: their sum, its product with every page's key sum, the top_k best, the list in order.
+// Scores are in 64 bits: a page's place must not hang on the order of a summation, and two scores that differ in exact
+// arithmetic hardly ever agree to 1e-16.  The key sums of a head (n_pages * D floats) are read by every tile, from the L2.
+constexpr int kSelThreads = 256;
+
+__device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below everything
+  if (isnan(x)) return 0ull;
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u >> 63 ? ~u : u | (1ull << 63);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c, RfQueries u, int keep_first, int keep_last, int top_k, int32_t* count,
+                                                                      int32_t* pages, int n_k, int32_t* dev_status) {
+  constexpr int kCols = D / 8, kGroups = kSelThreads / kCols, kPer = D / 32;
+  extern __shared__ uint64_t key[];                       // [pages of the sequence]
+  __shared__ double part[kGroups][D];
+  __shared__ double pooled[D];
+  __shared__ float tail_sum[D];
+  __shared__ int hist[256], state[4], warp_n[kSelThreads / 32][2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  rf_grid_trigger();
+  rf_grid_wait();
+  const int len = rf_seq_len(c, b, dev_status), q_len = rf_query_len(u, b, dev_status);
+  const int sees = rf_rows_see(u, len, q_len, tile * kPage, kPage);
+  const size_t row = ((size_t)b * c.H + h) * u.n_q + tile;
+  const int n = min(rf_pages(max(sees, 0)), kSelectMaxPages);
+  if (n == 0) {
+    if (tid == 0) count[row] = 0;
+    return;
+  }
+  const int first_end = min(keep_first, n), last_begin = max(n - min(keep_last, n), first_end);
+  const int rest = last_begin - first_end, best = min(top_k, rest);
+  uint64_t threshold = ~0ull;
+  int equal_allowed = 0;                                  // pages of exactly the threshold's score that are taken, lowest first
+  if (best > 0 && best < rest) {
+    {
+      const int col = tid % kCols, group = tid / kCols;
+      if (group < kGroups) {
+        double acc[8] = {};
+        const __nv_bfloat16* q = u.q + (((size_t)b * c.H + h) * u.rows) * D + col * 8;
+        for (int r = group; r < kPage; r += kGroups) {
+          const int at = tile * kPage + r;
+          if (at >= u.rows) break;
+          if (at % u.M >= q_len) continue;
+          const uint4 v = *reinterpret_cast<const uint4*>(q + (size_t)at * D);
+          const uint32_t* x = &v.x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[2 * i] += (double)__uint_as_float(x[i] << 16);
+            acc[2 * i + 1] += (double)__uint_as_float(x[i] & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[group][col * 8 + i] = acc[i];
+      }
+    }
+    __syncthreads();
+    if (tid < D) {
+      double s = 0.0;
+      for (int g = 0; g < kGroups; ++g) s += part[g][tid];
+      pooled[tid] = s;
+    }
+    __syncthreads();
+    // A last page that is not full is summed up from its codes: it may be part of a page that another sequence has filled
+    // further, or that was fuller when it was written.
+    const int tail = len % kPage != 0 && last_begin == rf_pages(len) ? last_begin - 1 : -1;
+    if (tail >= 0) {
+      const size_t side = (size_t)rf_page(c, b, tail, dev_status) * c.H + h;
+      const uint8_t* codes = c.k + side * kPage * D;
+      if (tid < D) {
+        int sum = 0;
+        for (int r = 0; r < len % kPage; ++r) sum += code_units(codes[r * D + tid]);
+        tail_sum[tid] = (float)sum * 0.001953125f * c.k_scale[side];
+      }
+      __syncthreads();
+    }
+    double p[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) p[i] = pooled[lane + 32 * i];
+    constexpr int kAhead = 4;                              // pages of a warp under way together
+    for (int c0 = first_end + warp; c0 < last_begin; c0 += kAhead * 8) {
+      float s[kAhead][kPer];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int col = c0 + 8 * j;
+        const float* x = c.k_sum + ((size_t)(col < last_begin ? rf_page(c, b, col, dev_status) : 0) * c.H + h) * D + lane;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) s[j][i] = col == tail ? tail_sum[lane + 32 * i] : x[32 * i];
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int col = c0 + 8 * j;
+        double d = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) d += p[i] * (double)s[j][i];
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
+        if (lane == 0 && col < last_begin) key[col] = ordered(d / (double)min(kPage, len - col * kPage));
+      }
+    }
+    // the best-th largest: eight bits at a time
+    uint64_t prefix = 0ull;
+    int need = best;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+      hist[tid] = 0;
+      __syncthreads();
+      for (int i = first_end + tid; i < last_begin; i += kSelThreads) {
+        const uint64_t k = key[i];
+        if (shift == 56 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(int)(k >> shift) & 255], 1);
+      }
+      __syncthreads();
+      if (warp == 0) {                                     // from the top bin down: where `need` is reached
+        int v[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[i] = hist[255 - (lane * 8 + i)];
+          sum += v[i];
+        }
+        int before = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, before, d);
+          if (lane >= d) before += y;
+        }
+        before -= sum;
+        if (before < need && before + sum >= need) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (before < need && before + v[i] >= need) {
+              state[0] = 255 - (lane * 8 + i);
+              state[1] = need - before;
+              state[2] = v[i];
+              break;
+            }
+            before += v[i];
+          }
+        }
+      }
+      __syncthreads();
+      prefix = prefix << 8 | (uint64_t)state[0];
+      need = state[1];
+      const int in_bin = state[2];
+      threshold = prefix << shift;
+      equal_allowed = need;
+      __syncthreads();
+      if (in_bin == need) {                                // the whole bin is taken: everything from its lower end on
+        equal_allowed = 0x7fffffff;
+        break;
+      }
+    }
+  } else if (best == rest) {
+    threshold = 0ull;
+    equal_allowed = 0x7fffffff;
+  }
+  // the list, in order
+  const bool scored = best > 0 && best < rest;
+  int out = 0, ties = 0;
+  for (int base = 0; base < n; base += kSelThreads) {
+    const int col = base + tid;
+    const bool always = col < n && (col < first_end || col >= last_begin);
+    const bool candidate = col < n && !always && best > 0;
+    const uint64_t k = candidate && scored ? key[col] : 0ull;
+    // (where the whole last bin is taken `threshold` is its lower end and equal_allowed has no bound)
+    const bool tie = candidate && scored && equal_allowed != 0x7fffffff && k == threshold;
+    const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
+    if (lane == 0) warp_n[warp][0] = __popc(tie_mask);
+    __syncthreads();
+    int tie_rank = ties + __popc(tie_mask & ((1u << lane) - 1u)), tie_all = 0;
+#pragma unroll
+    for (int i = 0; i < kSelThreads / 32; ++i) {
+      if (i < warp) tie_rank += warp_n[i][0];
+      tie_all += warp_n[i][0];
+    }
+    bool take = always;
+    if (candidate) take = !scored ? true : tie ? tie_rank < equal_allowed : equal_allowed == 0x7fffffff ? k >= threshold : k > threshold;
+    const uint32_t mask = __ballot_sync(0xffffffffu, take);
+    if (lane == 0) warp_n[warp][1] = __popc(mask);
+    __syncthreads();
+    int at = out + __popc(mask & ((1u << lane) - 1u)), all = 0;
+#pragma unroll
+    for (int i = 0; i < kSelThreads / 32; ++i) {
+      if (i < warp) at += warp_n[i][1];
+      all += warp_n[i][1];
+    }
+    if (take && at < n_k && rf_in_bounds(at, n_k, dev_status)) pages[row * n_k + at] = col;
+    out += all;
+    ties += tie_all;
+    __syncthreads();
+  }
+  if (tid == 0) count[row] = min(out, n_k);
+}
+
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || bytes <= 48 * 1024 || (dev < 64 && done[dev])) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  if (e == cudaSuccess && dev < 64) done[dev] = true;
+  return e;
+}
+
+}  // namespace
+
+size_t rf_cache_ws_words(const RfCache& c) { return kWsHead + 3 * (size_t)c.B + 2 * (size_t)c.n_pages; }
+
+cudaError_t rf_launch_cache_append(const RfCache& c, const __nv_bfloat16* k, const __nv_bfloat16* v, int M, const int32_t* new_len,
+                                   int32_t* ws, int32_t* dev_status, cudaStream_t st) {
+  static bool done[64] = {};
+  const size_t smem = 2 * sizeof(uint32_t) * rf_cdiv(c.n_pages, 32);
+  cudaError_t e = allow_smem(rf_cache_plan_kernel, smem, done);
+  if (e != cudaSuccess) return e;
+  e = rf_launch(rf_cache_plan_kernel, dim3(1), kPlanThreads, smem, st, c, M, new_len, ws, dev_status);
+  if (e != cudaSuccess) return e;
+  const dim3 grid((unsigned)((M - 1 + kPage - 1) / kPage + 1), c.H, 2 * c.B);   // pages that M tokens from any place on can touch
+  switch (c.D) {
+    case 64: return rf_launch(rf_cache_write_kernel<64>, grid, 128, 0, st, c, k, v, M, ws, dev_status);
+    case 96: return rf_launch(rf_cache_write_kernel<96>, grid, 192, 0, st, c, k, v, M, ws, dev_status);
+    default: return rf_launch(rf_cache_write_kernel<128>, grid, 256, 0, st, c, k, v, M, ws, dev_status);
+  }
+}
+
+cudaError_t rf_launch_cache_fork(const RfCache& c, const int32_t* parent, int32_t* dev_status, cudaStream_t st) {
+  static bool done[64] = {};
+  const size_t smem = (size_t)c.B * 33 * sizeof(int);
+  cudaError_t e = allow_smem(rf_cache_fork_kernel, smem, done);
+  if (e != cudaSuccess) return e;
+  return rf_launch(rf_cache_fork_kernel, dim3(rf_cdiv(c.max_pages, 32)), 256, smem, st, c, parent, dev_status);
+}
+
+cudaError_t rf_launch_cache_drop(const RfCache& c, const int32_t* first, const int32_t* count, const int32_t* max_len,
+                                 int32_t* dev_status, cudaStream_t st) {
+  return rf_launch(rf_cache_drop_kernel, dim3(c.B), 256, 0, st, c, first, count, max_len, dev_status);
+}
+
+cudaError_t rf_launch_cache_compact(const RfCache& c, int32_t* n_live, int32_t* ws, int32_t* dev_status, cudaStream_t st) {
+  static bool done[64] = {};
+  const size_t smem = sizeof(uint32_t) * rf_cdiv(c.n_pages, 32);
+  cudaError_t e = allow_smem(rf_cache_compact_plan_kernel, smem, done);
+  if (e != cudaSuccess) return e;
+  e = rf_launch(rf_cache_compact_plan_kernel, dim3(1), kPlanThreads, smem, st, c, n_live, ws, dev_status);
+  if (e != cudaSuccess) return e;
+  const long long most = (long long)c.n_pages * c.H;      // of n pages at most half move, two items a head
+  return rf_launch(rf_cache_move_kernel, dim3((unsigned)(most < 148 * 8 ? most : 148 * 8)), 256, 0, st, c, ws, dev_status);
+}
+
+cudaError_t rf_launch_cache_select(const RfCache& c, const RfQueries& u, int keep_first, int keep_last, int top_k, int32_t* count,
+                                   int32_t* pages, int n_k, int32_t* dev_status, cudaStream_t st) {
+  const size_t smem = sizeof(uint64_t) * (size_t)c.max_pages;
+  const dim3 grid(u.n_q, c.H, c.B);
+  auto go = [&](auto kernel, bool (&done)[64]) -> cudaError_t {
+    const cudaError_t e = allow_smem(kernel, smem + 32 * 1024, done);   // (the static arrays count too)
+    if (e != cudaSuccess) return e;
+    return rf_launch(kernel, grid, kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
+  };
+  static bool d64[64] = {}, d96[64] = {}, d128[64] = {};
+  switch (c.D) {
+    case 64: return go(rf_cache_select_kernel<64>, d64);
+    case 96: return go(rf_cache_select_kernel<96>, d96);
+    default: return go(rf_cache_select_kernel<128>, d128);
+  }
+}

@@ -1,0 +1,442 @@
+// Attention over the paged 8-bit cache for few query rows (single tokens; the rows of all query heads that share a K/V head).
+//
+// o = softmax(scale q k^T) v, over the keys that each row sees.  Every K and V byte is used by at most 16 rows, so the floor is
+// the cache's bytes at the HBM rate: an SM has 1400 cycles for the 32 KB of a tile of 128 keys at D = 128.
+// A producer warp streams the tiles into a ring in shared memory by TMA (page by page, swizzled, 128 KB under way); eight warps
+// take 16 keys of a tile each: S = q K^T and O += P V on mma.sync (16 rows x 8 keys x 16; the tensor pipe idles at any rate here,
+// and a tcgen05 tile is 128 rows), codes widened to bf16 in registers, exactly.  The order of a contraction is free, so the
+// words are used as they lie: K's four bytes of a word are four of the 16 terms of one instruction, and V's bytes of two
+// keys are brought together by one byte permutation.  Each warp keeps its own maxima and sums (fp32); they meet once per item.
+#include <algorithm>
+
+#include "rf_cache_attn.cuh"
+
+using namespace sm100;
+using namespace rf_cache_attn;
+
+namespace {
+
+constexpr int kRows = 16, kWarps = 8, kThreads = 32 * (kWarps + 1);
+enum { kFirst = 1, kLast = 2, kNothing = 4, kHeadPiece = 8, kTailPiece = 16, kEnd = 32 };
+
+template <int D>
+struct Cfg {
+  static constexpr int PITCH = D == 64 ? 64 : 128;                  // bytes of a row in shared memory
+  static constexpr uint32_t TILE = kPage * PITCH;
+  static constexpr int STAGES = D == 64 ? 8 : 4;
+  static constexpr uint32_t JOIN = STAGES * 2 * TILE;               // [kWarps][kRows][D] float
+  static constexpr uint32_t SUMS = JOIN + kWarps * kRows * D * 4;   // [kWarps][kRows] {m, l, l of the unrounded weights}
+  static constexpr uint32_t BAR = SUMS + kWarps * kRows * 16;
+  static constexpr uint32_t REC = BAR + 8 * (2 * STAGES + 2);
+  static constexpr uint32_t MISC = REC + STAGES * 32;
+  static constexpr uint32_t TOTAL = MISC + 16 + sizeof(StretchScratch);
+  static constexpr uint32_t ALLOC = TOTAL + 1024;
+  static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
+  static constexpr int PIECE = kRows * (D + 4);                     // floats: O [kRows][D], then {m, l, l exact, 0} per row
+  // byte offset of 16-byte chunk c of row r
+  static __device__ __forceinline__ uint32_t chunk(int r, int c) {
+    return r * PITCH + ((D == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4);
+  }
+};
+
+struct Record { int item, page, flags; uint32_t k1, k2, v1, v2; int pad; };
+
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+struct Maps { CUtensorMap k, v; };
+
+template <int D, bool LSE>
+__global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  auto full = [&](int s) -> uint32_t { return base + C::BAR + 8u * s; };
+  auto empty = [&](int s) -> uint32_t { return base + C::BAR + 8u * (C::STAGES + s); };
+  const uint32_t joined = base + C::BAR + 8u * (2 * C::STAGES), read = joined + 8;   // all pieces of an item are in shared memory; they have been read
+  volatile Record* records = reinterpret_cast<volatile Record*>(base_ptr + C::REC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC);
+  StretchScratch* scratch = reinterpret_cast<StretchScratch*>(base_ptr + C::MISC + 16);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kWarps); }
+    mbar_init(joined, kWarps);
+    mbar_init(read, kWarps);
+    *abort_flag = 0;
+    mbar_init_fence();
+  }
+  if (tid == 32 * kWarps) { prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
+  rf_grid_trigger();
+  rf_grid_wait();
+  const Stretch st = stretch<kRows, kThreads>(a, scratch);      // (its barriers also publish the mbarriers)
+  const WaitCtx wc{abort_flag, a.dev_status};
+  if (tid == 0) {
+    int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
+    head[0] = st.item;
+    head[1] = (int)(uint32_t)(st.at & 0xffffffffll);
+    head[2] = (int)(st.at >> 32);
+    head[3] = st.lo < st.hi && st.at < st.lo;
+  }
+
+  if (warp == kWarps) {
+    // ------------------------------------------------------------ producer
+    int stage = 0, item = st.item;
+    uint32_t phase = 1;                       // of the empty barriers: the first round finds them free
+    long long at = st.at;
+    auto publish = [&](const Record& r, bool bytes, int row) {   // lane 0
+      if (!mbar_wait(empty(stage), phase, wc)) return;            // abandoned: nothing more is fetched
+      volatile Record* d = records + stage;
+      d->item = r.item; d->page = r.page; d->flags = r.flags;
+      d->k1 = r.k1; d->k2 = r.k2; d->v1 = r.v1; d->v2 = r.v2;
+      if (bytes) {
+        const uint32_t to = base + stage * 2 * C::TILE;
+        mbar_expect_tx(full(stage), 2 * C::TILE);
+        tma_load_3d(to, &maps.k, 0, 0, row, full(stage));
+        tma_load_3d(to + C::TILE, &maps.v, 0, 0, row, full(stage));
+      } else {
+        mbar_arrive(full(stage));
+      }
+    };
+    auto step = [&]() {
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+    };
+    for (long long pos = st.lo; pos < st.hi; ++item) {
+      const CacheItem it = cache_item<kRows>(a, item);
+      const int tiles = item_tiles<kRows>(a, it), n = places(tiles);
+      if (n == 0) continue;
+      const int begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+      const int cut = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
+      const int32_t* list = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
+      const int pages = rf_pages(it.len);
+      for (int t0 = begin; t0 < end; t0 += 32) {
+        // a batch of tiles' entries, pages and scales: a lane each
+        Record r;
+        const int t = t0 + lane;
+        int row = 0;
+        r.item = item;
+        r.page = t;
+        r.flags = cut | (t == begin ? kFirst : 0) | (t == end - 1 ? kLast : 0);
+        r.k1 = r.k2 = r.v1 = r.v2 = 0u;
+        if (t < end && t < tiles) {
+          if (list != nullptr) r.page = list[t];
+          if (r.page < 0 || r.page >= pages) {
+            rf_report(a.dev_status, RF_ERR_INVALID_ARG);
+            r.flags |= kNothing;
+          } else {
+            row = rf_page(a.c, it.b, r.page, a.dev_status) * a.c.H + it.bh % a.c.H;
+            const Widen k = widen_by(a.c.k_scale[row]), v = widen_by(a.c.v_scale[row]);
+            r.k1 = k.m1; r.k2 = k.m2; r.v1 = v.m1; r.v2 = v.m2;
+          }
+        } else {
+          r.flags |= kNothing;
+        }
+        const int batch = min(32, end - t0);
+        for (int i = 0; i < batch; ++i) {
+          Record s;
+          s.item = item;
+          s.page = __shfl_sync(0xffffffffu, r.page, i);
+          s.flags = __shfl_sync(0xffffffffu, r.flags, i);
+          s.k1 = __shfl_sync(0xffffffffu, r.k1, i);
+          s.k2 = __shfl_sync(0xffffffffu, r.k2, i);
+          s.v1 = __shfl_sync(0xffffffffu, r.v1, i);
+          s.v2 = __shfl_sync(0xffffffffu, r.v2, i);
+          const int row_i = __shfl_sync(0xffffffffu, row, i);
+          if (lane == 0) publish(s, !(s.flags & kNothing), row_i);
+          __syncwarp();
+          step();
+        }
+      }
+      at += n;
+      pos = at;
+    }
+    if (lane == 0) publish(Record{0, 0, kEnd, 0, 0, 0, 0, 0}, false, 0);
+  } else {
+    // ------------------------------------------------------------ consumers: 16 keys of every tile each
+    const int g = lane >> 2, t = lane & 3;
+    uint32_t q[D / 16][4];
+    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, lx[2] = {0.f, 0.f};
+    int sees[2] = {0, 0};
+    uint32_t item_no = 0;
+    CacheItem it = {};
+    int stage = 0;
+    uint32_t phase = 0;
+    for (;;) {
+      // (the warp as a whole: after an abandoned wait its lanes may differ in what they saw)
+      if (!__all_sync(0xffffffffu, mbar_wait_long(full(stage), phase, wc, 0))) break;
+      Record rec;
+      {
+        volatile const Record* r = records + stage;
+        rec.item = r->item; rec.page = r->page; rec.flags = r->flags;
+        rec.k1 = r->k1; rec.k2 = r->k2; rec.v1 = r->v1; rec.v2 = r->v2;
+      }
+      if (rec.flags & kEnd) break;
+      if (rec.flags & kFirst) {
+        it = cache_item<kRows>(a, rec.item);
+        const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = it.r0 + g + 8 * i, place = r % a.u.M;
+          const bool there = r < a.u.rows && place < it.q_len;
+          sees[i] = there ? rf_row_sees(a.u.causal, it.len, it.q_len, place) : 0;
+          m[i] = -INFINITY;
+          l[i] = lx[i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            uint2 x = make_uint2(0u, 0u);
+            if (there) x = *reinterpret_cast<const uint2*>(src + (size_t)r * D + 16 * ks + 4 * t);
+            q[ks][i] = __byte_perm(x.x, x.y, 0x7632);          // columns 1 and 3 of the four, as widen_odd gives the keys'
+            q[ks][2 + i] = __byte_perm(x.x, x.y, 0x5410);      // columns 0 and 2
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+      }
+      if (!(rec.flags & kNothing)) {
+        const uint32_t kt = base + stage * 2 * C::TILE, vt = kt + C::TILE;
+        float s[2][4] = {};
+        const bool twice = rec.k2 != kOne2 || rec.v2 != kOne2;
+        {
+          const int row = 16 * warp + (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ks += 2) {
+            uint32_t x[4];
+            ldmatrix4(kt + C::chunk(row, ks + c0), x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                       // keys 0-7: chunks ks, ks + 1; keys 8-15 likewise
+              uint32_t hi = mul_bf16x2(widen_odd(x[i]), rec.k1), lo = mul_bf16x2(widen_even(x[i]), rec.k1);
+              if (twice) { hi = mul_bf16x2(hi, rec.k2); lo = mul_bf16x2(lo, rec.k2); }
+              const int k = ks + (i & 1);
+              mma16816(s[i >> 1], q[k][0], q[k][1], q[k][2], q[k][3], hi, lo);
+            }
+          }
+        }
+        // scores to weights; key 8 nb + 2 t + e of this warp's sixteen, rows g and g + 8
+        const int key0 = rec.page * kPage + 16 * warp + 2 * t;
+        float alpha[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float& x = s[nb][2 * i + e];
+              x = key0 + 8 * nb + e < sees[i] ? x * a.scale_log2 : -INFINITY;
+              mx = fmaxf(mx, x);
+            }
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float m_new = fmaxf(m[i], mx), use = m_new == -INFINITY ? 0.f : m_new;
+          alpha[i] = m_new == m[i] ? 1.f : ex2(m[i] - use);      // 0 from -inf on
+          m[i] = m_new;
+          float sum = 0.f, sumx = 0.f;
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) {
+            const float p0 = ex2(s[nb][2 * i] - use), p1 = ex2(s[nb][2 * i + 1] - use);
+            const uint32_t pk = pack_bf16(p0, p1);               // P V multiplies the rounded weights: they normalise O
+            sum += __uint_as_float(pk << 16) + __uint_as_float(pk & 0xffff0000u);
+            if (LSE) sumx += p0 + p1;
+            s[nb][2 * i] = __uint_as_float(pk);
+          }
+          l[i] = l[i] * alpha[i] + sum;
+          if (LSE) lx[i] = lx[i] * alpha[i] + sumx;
+        }
+        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) { o[n][0] *= alpha[0]; o[n][1] *= alpha[0]; o[n][2] *= alpha[1]; o[n][3] *= alpha[1]; }
+        }
+        const uint32_t p0 = __float_as_uint(s[0][0]), p1 = __float_as_uint(s[0][2]), p2 = __float_as_uint(s[1][0]), p3 = __float_as_uint(s[1][2]);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+          // word g + 8 j of keys 2t, 2t+1, 2t+8, 2t+9: columns 4 (g + 8 j) .. + 3
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = lds32(vt + C::chunk(16 * warp + 2 * t + (i & 1) + 8 * (i >> 1), 2 * j + (g >> 2)) + (g & 3) * 4);
+#pragma unroll
+          for (int hlf = 0; hlf < 2; ++hlf) {
+            const uint32_t y = __byte_perm(w[0], w[1], hlf ? 0x7632 : 0x5410), z = __byte_perm(w[2], w[3], hlf ? 0x7632 : 0x5410);
+            uint32_t ye = mul_bf16x2(widen_even(y), rec.v1), ze = mul_bf16x2(widen_even(z), rec.v1);
+            uint32_t yo = mul_bf16x2(widen_odd(y), rec.v1), zo = mul_bf16x2(widen_odd(z), rec.v1);
+            if (twice) {
+              ye = mul_bf16x2(ye, rec.v2); ze = mul_bf16x2(ze, rec.v2);
+              yo = mul_bf16x2(yo, rec.v2); zo = mul_bf16x2(zo, rec.v2);
+            }
+            mma16816(o[4 * j + 2 * hlf], p0, p1, p2, p3, ye, ze);
+            mma16816(o[4 * j + 2 * hlf + 1], p0, p1, p2, p3, yo, zo);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(stage));
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      if (!(rec.flags & kLast)) continue;
+
+      // ---------------------------------------------------------- the item's (or piece's) end: the eight warps' rows meet
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 1; d < 4; d <<= 1) {
+          l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+          if (LSE) lx[i] += __shfl_xor_sync(0xffffffffu, lx[i], d);
+        }
+      }
+      const int n_rows = min(kRows, a.u.rows - it.r0);
+      float* buf = reinterpret_cast<float*>(base_ptr + C::JOIN);
+      float4* sums = reinterpret_cast<float4*>(base_ptr + C::SUMS);
+      if (item_no > 0) mbar_wait(read, (item_no - 1) & 1, wc);    // the item before has been read
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = g + 8 * i;
+        if (r >= n_rows) continue;
+        if (t == 0) sums[warp * kRows + r] = make_float4(m[i], l[i], lx[i], 0.f);
+        float* row = buf + ((size_t)warp * kRows + r) * D;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            *reinterpret_cast<float4*>(row + 4 * (2 * t + e + 8 * j)) =
+                make_float4(o[4 * j][2 * i + e], o[4 * j + 1][2 * i + e], o[4 * j + 2][2 * i + e], o[4 * j + 3][2 * i + e]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(joined);
+      mbar_wait(joined, item_no & 1, wc);
+      ++item_no;
+      const bool piece = rec.flags & (kHeadPiece | kTailPiece);
+      float* slot = a.ws + head_floats(gridDim.x) + ((size_t)2 * blockIdx.x + (rec.flags & kTailPiece ? 1 : 0)) * C::PIECE;
+      for (int i = tid; i < n_rows * (D / 4); i += 32 * kWarps) {
+        const int r = i / (D / 4), d4 = i % (D / 4), place = (it.r0 + r) % a.u.M;
+        float mm = -INFINITY, ll = 0.f, llx = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sums[w * kRows + r].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float use = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 sm = sums[w * kRows + r], x = *reinterpret_cast<const float4*>(buf + ((size_t)w * kRows + r) * D + d4 * 4);
+          const float f = ex2(sm.x - use);
+          ll += sm.y * f; llx += sm.z * f;
+          acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+        }
+        if (piece) {
+          __stcg(reinterpret_cast<float4*>(slot + (size_t)r * D) + d4, acc);
+          if (d4 == 0) __stcg(reinterpret_cast<float4*>(slot + (size_t)kRows * D) + r, make_float4(mm, ll, llx, 0.f));
+        } else if (place < it.q_len) {
+          const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);   // (a sum that is no number stays one)
+          const size_t at_row = (size_t)it.bh * a.u.rows + it.r0 + r;
+          *reinterpret_cast<uint2*>(a.o + at_row * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+          if (LSE && d4 == 0) a.lse[at_row] = (mm + log2f(llx)) * 0.6931471805599453f;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(read);
+    }
+  }
+  __syncthreads();
+  if (tid == 0 && *abort_flag) __nanosleep(20000);   // let abandoned copies land before shared memory is released
+}
+
+// Joins the pieces of the items that the stretches cut.  CTA x looks at the cut between stretches x and x + 1 and works if it is the
+// first one inside its item; blockIdx.y is the row.
+template <int D, bool LSE>
+__global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant__ RfCacheAttn a, int ctas) {
+  constexpr int PIECE = Cfg<D>::PIECE;
+  __shared__ float red[2][D / 32];
+  extern __shared__ float weight[];              // [ctas]
+  rf_grid_trigger();
+  rf_grid_wait();
+  const int x = blockIdx.x + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y;
+  const int32_t* heads = reinterpret_cast<const int32_t*>(a.ws);
+  const int32_t* mine = heads + x * kHeadWords;
+  if (!mine[3]) return;
+  // the item begins in the stretch before, unless that one begins inside it too
+  const int32_t* prev = mine - kHeadWords;
+  if (prev[3] && prev[0] == mine[0]) return;
+  int n = 1;                                     // stretches x .. x + n - 1 begin inside the item
+  while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
+  const CacheItem it = cache_item<kRows>(a, mine[0]);
+  const int row = it.r0 + r;
+  if (row >= a.u.rows || row % a.u.M >= it.q_len) return;
+  const float* pieces = a.ws + head_floats(ctas);
+  // piece 0 is the one that stretch x - 1 ends in, piece i > 0 the one that stretch x + i - 1 begins in
+  auto at = [&](int i) -> const float* { return pieces + (i == 0 ? (size_t)2 * (x - 1) + 1 : (size_t)2 * (x + i - 1)) * PIECE; };
+  float mm = -INFINITY;
+  for (int i = tid; i <= n; i += D) {
+    const float m = __ldcg(at(i) + (size_t)kRows * D + r * 4);
+    weight[i] = m;
+    mm = fmaxf(mm, m);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+  if (lane == 0) red[0][warp] = mm;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) mm = fmaxf(mm, red[0][i]);
+  const float use = mm == -INFINITY ? 0.f : mm;
+  float l = 0.f, lx = 0.f, acc = 0.f;
+#pragma unroll 4
+  for (int i = 0; i <= n; ++i) {
+    const float4 sm = __ldcg(reinterpret_cast<const float4*>(at(i) + (size_t)kRows * D) + r);
+    const float f = ex2(weight[i] - use);
+    l += sm.y * f;
+    lx += sm.z * f;
+    acc += __ldcg(at(i) + (size_t)r * D + tid) * f;
+  }
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+  const size_t at_row = (size_t)it.bh * a.u.rows + row;
+  a.o[at_row * D + tid] = __float2bfloat16_rn(acc * inv);
+  if (LSE && tid == 0) a.lse[at_row] = (mm + log2f(lx)) * 0.6931471805599453f;
+}
+
+// One CTA an SM; fewer where there is nothing to share out (a bound on the places of the line from the sizes alone).
+int token_ctas(const RfCache& c, const RfQueries& u) {
+  const long long items = (long long)c.B * c.H * rf_cdiv(u.rows, kRows), most = items * std::max(c.max_pages, 1);
+  return (int)std::min<long long>(most, 148);
+}
+
+template <int D, bool LSE>
+rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
+  using C = Cfg<D>;
+  static bool configured[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return RF_ERR_CUDA;
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    if (cudaFuncSetAttribute(rf_cache_token_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::ALLOC) != cudaSuccess)
+      return RF_ERR_CUDA;
+    configured[dev] = true;
+  }
+  Maps maps;
+  if (!rf_encode_pages_map(&maps.k, a.c.k, a.c) || !rf_encode_pages_map(&maps.v, a.c.v, a.c)) return RF_ERR_CUDA;
+  const int ctas = token_ctas(a.c, a.u);
+  if (rf_launch(rf_cache_token_kernel<D, LSE>, dim3(ctas), kThreads, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
+  if (ctas == 1) return RF_OK;
+  const dim3 grid(ctas - 1, std::min(kRows, a.u.rows));
+  return rf_launch(rf_cache_join_kernel<D, LSE>, grid, D, sizeof(float) * (ctas + 1), st, a, ctas) == cudaSuccess ? RF_OK : RF_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t rf_cache_attn_ws_bytes(const RfCache& c, const RfQueries& u) {
+  const int ctas = token_ctas(c, u);
+  return (head_floats(ctas) + (size_t)2 * ctas * kRows * (c.D + 4)) * sizeof(float);
+}
+
+rf_status rf_launch_cache_attn(const RfCacheAttn& a, cudaStream_t st) {
+  const bool lse = a.lse != nullptr;
+  switch (a.c.D) {
+    case 64: return lse ? launch<64, true>(a, st) : launch<64, false>(a, st);
+    case 96: return lse ? launch<96, true>(a, st) : launch<96, false>(a, st);
+    case 128: return lse ? launch<128, true>(a, st) : launch<128, false>(a, st);
+  }
+  return RF_ERR_UNSUPPORTED;
+}

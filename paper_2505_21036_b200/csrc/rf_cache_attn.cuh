@@ -1,0 +1,117 @@
+// What the attention kernels over the cache share: how the work is cut, how pieces are left and joined, how codes are widened.
+//
+// The work of a call is one line of key tiles: the items (a K/V head's block of query rows) one after another, each with the
+// tiles that it lists.  The line is cut into as many equal stretches as there are CTAs, wherever that falls, so every SM gets
+// the same number of tiles whatever the lengths are; an item that is cut leaves unnormalised pieces in the workspace, which
+// a second kernel joins in order.  Lengths and lists are on the device, so every CTA sums the items up for itself.
+#pragma once
+
+#include "rf_cache.cuh"
+#include "rf_sm100.cuh"
+
+namespace rf_cache_attn {
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// An item: rows [r0, r0 + kRows) of K/V head bh.
+struct CacheItem { int b, bh, r0, len, q_len, sees; };
+template <int kRows>
+__device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
+  const int blocks = rf_cdiv(a.u.rows, kRows);
+  CacheItem it;
+  it.bh = item / blocks;
+  it.r0 = (item - it.bh * blocks) * kRows;
+  it.b = it.bh / a.c.H;
+  it.len = rf_seq_len(a.c, it.b, a.dev_status);
+  it.q_len = rf_query_len(a.u, it.b, a.dev_status);
+  it.sees = rf_rows_see(a.u, it.len, it.q_len, it.r0, kRows);
+  return it;
+}
+// Entries of the list of a tile of query rows.
+__device__ __forceinline__ int listed(const RfCacheAttn& a, int bh, int tile) {
+  return min(max(a.count[(size_t)bh * a.u.n_q + tile], 0), a.n_k);
+}
+// Key tiles that the item walks: its places on the line.  -1: all of its rows are padding.
+template <int kRows>
+__device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem& it) {
+  if (it.sees < 0) return -1;
+  if (a.count == nullptr) return rf_pages(it.sees);
+  int n = listed(a, it.bh, it.r0 / kPage);
+  if (kRows > kPage && it.r0 / kPage + 1 < a.u.n_q) n = max(n, listed(a, it.bh, it.r0 / kPage + 1));
+  return n;
+}
+// A row block that sees nothing has a place on the line too: its outputs are written.
+__device__ __forceinline__ int places(int tiles) { return tiles < 0 ? 0 : max(tiles, 1); }
+
+// A CTA's stretch [lo, hi) of the line, and the item that lo lies in (which begins at place `at`).
+struct Stretch { long long lo, hi, at; int item; };
+struct StretchScratch { long long sums[33]; Stretch st; };
+
+// Called by all threads of the CTA (kThreads of them, whole warps).
+template <int kRows, int kThreads>
+__device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch* s) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int items = a.c.B * a.c.H * rf_cdiv(a.u.rows, kRows), per = rf_cdiv(items, kThreads);
+  const int i0 = min(tid * per, items), i1 = min(i0 + per, items);
+  long long mine = 0;
+  for (int i = i0; i < i1; ++i) mine += places(item_tiles<kRows>(a, cache_item<kRows>(a, i)));
+  long long x = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 31) s->sums[warp] = x;
+  __syncthreads();
+  long long before = x - mine, total = 0;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += s->sums[w];
+    total += s->sums[w];
+  }
+  // no more stretches than places: the ones in use are the first, and none of them is empty
+  const long long n = min((long long)gridDim.x, max(total, 1ll)), x0 = min((long long)blockIdx.x, n), x1 = min(x0 + 1, n);
+  const long long lo = total * x0 / n, hi = total * x1 / n;
+  if (tid == 0 && lo == hi) s->st = Stretch{lo, hi, lo, items};
+  if (lo < hi && before <= lo && lo < before + mine) {
+    long long at = before;
+    int i = i0;
+    for (;; ++i) {
+      const int p = places(item_tiles<kRows>(a, cache_item<kRows>(a, i)));
+      if (lo < at + p) break;
+      at += p;
+    }
+    s->st = Stretch{lo, hi, at, i};
+  }
+  __syncthreads();
+  return s->st;
+}
+
+// Workspace: a head per CTA {item, its first place (two words), whether the CTA's stretch begins inside it}, then two
+// pieces per CTA: that of the item its stretch begins inside, that of the item its stretch ends inside.
+constexpr int kHeadWords = 4;
+__host__ __device__ __forceinline__ size_t head_floats(int ctas) { return ((size_t)ctas * kHeadWords + 63) / 64 * 64; }
+
+// Four codes of a word as two pairs of bf16: byte 1 and byte 3, byte 0 and byte 2.  A code's exponent lands eight bits too low
+// for a bf16's bias (by 2^-120, subnormal codes included, as both count their mantissa from the same place), so a product with
+// 2^120 times the page's scale, exact, makes it the stored value.  Seven integer instructions and two products for four codes.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t widen_odd(uint32_t x) { return ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u); }
+__device__ __forceinline__ uint32_t widen_even(uint32_t x) { return ((x << 4) & 0x07f007f0u) | ((x << 8) & 0x80008000u); }
+// The factors as bf16 pairs: 2^(120 + e) for the scale 2^e, in two steps where that is past bf16's exponents (e > 7).
+struct Widen { uint32_t m1, m2; };
+__device__ __forceinline__ Widen widen_by(float scale) {
+  const int e = min(max((int)((__float_as_uint(scale) >> 23) & 255u) - 127, -100), 100);
+  const uint32_t m1 = (uint32_t)(min(e, 7) + 120 + 127) << 7, m2 = (uint32_t)(max(e - 7, 0) + 127) << 7;
+  return Widen{m1 * 0x10001u, m2 * 0x10001u};
+}
+constexpr uint32_t kOne2 = 0x3f803f80u;   // m2 of e <= 7
+
+}  // namespace rf_cache_attn
