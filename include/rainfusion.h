@@ -426,7 +426,7 @@ rf_status rf_cache_compact(const rf_cache *cache, int32_t *n_live, void *ws, siz
 typedef struct {
   int32_t H, M;              /* query heads; rows of q per head */
   int32_t causal_block;      /* >= 0 */
-  float   scale;             /* of q k^T before the softmax; 0: 1 / sqrt(D) */
+  float   scale;             /* of q k^T before the softmax, > 0; 0 stands for 1 / sqrt(D) */
 } rf_cache_query;
 
 /*

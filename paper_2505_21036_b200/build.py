@@ -14,8 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librainfusion.so")
 LIB_CHECKED = os.path.join(PKG, "librainfusion_checked.so")
-SOURCES = ["rf_api.cu", "rf_mask.cu", "rf_arm.cu", "rf_attn.cu", "rf_host.cu", "rf_cache.cu", "rf_cache_attn.cu", "rf_cache_api.cu"]
-HEADERS = ["rf_common.cuh", "rf_decide.cuh", "rf_sm100.cuh", "rf_attn_common.cuh", "rf_cache.cuh", "rf_cache_attn.cuh", os.path.join("..", "..", "include", "rainfusion.h")]
+SOURCES = ["rf_api.cu", "rf_mask.cu", "rf_arm.cu", "rf_attn.cu", "rf_host.cu", "rf_cache.cu", "rf_cache_attn.cu", "rf_cache_chunk.cu", "rf_cache_api.cu"]
+HEADERS = ["rf_common.cuh", "rf_decide.cuh", "rf_sm100.cuh", "rf_attn_common.cuh", "rf_cache.cuh", "rf_cache_attn.cuh", "rf_attn_softmax.cuh", os.path.join("..", "..", "include", "rainfusion.h")]
 
 
 def nvcc_path() -> str:

@@ -94,4 +94,6 @@ struct RfCacheAttn {
 // D = 64; at D = 96 a row takes 128 bytes in shared memory, the last 32 of them zeros).
 bool rf_encode_pages_map(CUtensorMap* m, const uint8_t* codes, const RfCache& c);
 size_t rf_cache_attn_ws_bytes(const RfCache& c, const RfQueries& u);
+size_t rf_cache_chunk_ws_bytes(const RfCache& c, const RfQueries& u);
+rf_status rf_launch_cache_chunk(const RfCacheAttn& a, cudaStream_t st);
 rf_status rf_launch_cache_attn(const RfCacheAttn& a, cudaStream_t st);

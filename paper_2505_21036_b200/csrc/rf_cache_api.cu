@@ -22,7 +22,7 @@ rf_status check_cache(const rf_cache* c, RfCache* out) {
 }
 
 rf_status check_query(const RfCache& c, const rf_cache_query* u, RfQueries* out) {
-  if (u == nullptr || u->H < 1 || u->M < 1 || u->causal_block < 0 || !isfinite(u->scale) || u->H % c.H != 0) return RF_ERR_INVALID_ARG;
+  if (u == nullptr || u->H < 1 || u->M < 1 || u->causal_block < 0 || !(u->scale >= 0.f && isfinite(u->scale)) || u->H % c.H != 0) return RF_ERR_INVALID_ARG;
   const long long rows = (long long)(u->H / c.H) * u->M;
   if (rows > (1ll << 30) || (long long)c.B * c.H * ((rows + 15) / 16) > (1ll << 30)) return RF_ERR_UNSUPPORTED;
   *out = RfQueries{u->M, u->H / c.H, (int)rows, (int)((rows + kPage - 1) / kPage), u->causal_block, nullptr, nullptr};

@@ -54,6 +54,16 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Key tiles that an item walks; -1: all of its rows are padding.
+__device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem& it) {
+  if (it.sees < 0) return -1;
+  return a.count == nullptr ? rf_pages(it.sees) : listed(a, it, it.r0 / kPage);
+}
+struct TokenPlaces {
+  static constexpr int kRowsOf = kRows;
+  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) { return places(item_tiles(a, cache_item<kRows>(a, item))); }
+};
+
 struct Maps { CUtensorMap k, v; };
 
 template <int D, bool LSE>
@@ -79,13 +89,11 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
   if (tid == 32 * kWarps) { prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
   rf_grid_trigger();
   rf_grid_wait();
-  const Stretch st = stretch<kRows, kThreads>(a, scratch);      // (its barriers also publish the mbarriers)
+  const Stretch st = stretch<TokenPlaces, kThreads>(a, scratch);      // (its barriers also publish the mbarriers)
   const WaitCtx wc{abort_flag, a.dev_status};
   if (tid == 0) {
     int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
     head[0] = st.item;
-    head[1] = (int)(uint32_t)(st.at & 0xffffffffll);
-    head[2] = (int)(st.at >> 32);
     head[3] = st.lo < st.hi && st.at < st.lo;
   }
 
@@ -113,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
     };
     for (long long pos = st.lo; pos < st.hi; ++item) {
       const CacheItem it = cache_item<kRows>(a, item);
-      const int tiles = item_tiles<kRows>(a, it), n = places(tiles);
+      const int tiles = item_tiles(a, it), n = places(tiles);
       if (n == 0) continue;
       const int begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
       const int cut = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
@@ -426,12 +434,19 @@ rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
 
 }  // namespace
 
+namespace {
+// Whether a call's query rows are few: see the top of this file and of rf_cache_chunk.cu.
+bool few_rows(const RfQueries& u) { return u.rows <= kRows; }
+}  // namespace
+
 size_t rf_cache_attn_ws_bytes(const RfCache& c, const RfQueries& u) {
+  if (!few_rows(u)) return rf_cache_chunk_ws_bytes(c, u);
   const int ctas = token_ctas(c, u);
   return (head_floats(ctas) + (size_t)2 * ctas * kRows * (c.D + 4)) * sizeof(float);
 }
 
 rf_status rf_launch_cache_attn(const RfCacheAttn& a, cudaStream_t st) {
+  if (!few_rows(a.u)) return rf_launch_cache_chunk(a, st);
   const bool lse = a.lse != nullptr;
   switch (a.c.D) {
     case 64: return lse ? launch<64, true>(a, st) : launch<64, false>(a, st);

@@ -32,17 +32,8 @@ __device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) 
   return it;
 }
 // Entries of the list of a tile of query rows.
-__device__ __forceinline__ int listed(const RfCacheAttn& a, int bh, int tile) {
-  return min(max(a.count[(size_t)bh * a.u.n_q + tile], 0), a.n_k);
-}
-// Key tiles that the item walks: its places on the line.  -1: all of its rows are padding.
-template <int kRows>
-__device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem& it) {
-  if (it.sees < 0) return -1;
-  if (a.count == nullptr) return rf_pages(it.sees);
-  int n = listed(a, it.bh, it.r0 / kPage);
-  if (kRows > kPage && it.r0 / kPage + 1 < a.u.n_q) n = max(n, listed(a, it.bh, it.r0 / kPage + 1));
-  return n;
+__device__ __forceinline__ int listed(const RfCacheAttn& a, const CacheItem& it, int tile) {
+  return it.len == 0 ? 0 : min(max(a.count[(size_t)it.bh * a.u.n_q + tile], 0), a.n_k);
 }
 // A row block that sees nothing has a place on the line too: its outputs are written.
 __device__ __forceinline__ int places(int tiles) { return tiles < 0 ? 0 : max(tiles, 1); }
@@ -51,14 +42,14 @@ __device__ __forceinline__ int places(int tiles) { return tiles < 0 ? 0 : max(ti
 struct Stretch { long long lo, hi, at; int item; };
 struct StretchScratch { long long sums[33]; Stretch st; };
 
-// Called by all threads of the CTA (kThreads of them, whole warps).
-template <int kRows, int kThreads>
+// Called by all threads of the CTA (kThreads of them, whole warps).  Places::of(a, item): the item's places on the line.
+template <typename Places, int kThreads>
 __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch* s) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int items = a.c.B * a.c.H * rf_cdiv(a.u.rows, kRows), per = rf_cdiv(items, kThreads);
+  const int items = a.c.B * a.c.H * rf_cdiv(a.u.rows, Places::kRowsOf), per = rf_cdiv(items, kThreads);
   const int i0 = min(tid * per, items), i1 = min(i0 + per, items);
   long long mine = 0;
-  for (int i = i0; i < i1; ++i) mine += places(item_tiles<kRows>(a, cache_item<kRows>(a, i)));
+  for (int i = i0; i < i1; ++i) mine += Places::of(a, i);
   long long x = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -80,7 +71,7 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
     long long at = before;
     int i = i0;
     for (;; ++i) {
-      const int p = places(item_tiles<kRows>(a, cache_item<kRows>(a, i)));
+      const int p = Places::of(a, i);
       if (lo < at + p) break;
       at += p;
     }
@@ -90,7 +81,7 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
   return s->st;
 }
 
-// Workspace: a head per CTA {item, its first place (two words), whether the CTA's stretch begins inside it}, then two
+// Workspace: a head per CTA {the item its stretch begins in, -, -, whether it begins inside it}, then two
 // pieces per CTA: that of the item its stretch begins inside, that of the item its stretch ends inside.
 constexpr int kHeadWords = 4;
 __host__ __device__ __forceinline__ size_t head_floats(int ctas) { return ((size_t)ctas * kHeadWords + 63) / 64 * 64; }

@@ -1,0 +1,791 @@
+// Attention over the paged 8-bit cache for chunks of query rows, on tcgen05 / TMEM / TMA.
+//
+// o = softmax(scale q k^T) v over the keys that each row sees.  From some dozens of rows on the products bound it, not the
+// cache's bytes.  An item is 256 query rows of one K/V head in two tiles of 128 (two "streams"), as in the attention
+// kernel over whole clips, whose softmax it shares; what differs is where K and V come from.  They lie in pages, as codes:
+// four warps load a tile's codes, widen them to bf16 (exact, see widen_odd) and lay them out in shared memory in the swizzled
+// form that tcgen05 reads.  A tile of 128 keys is widened once for its 256 rows: 32 768 codes at 2.5 integer instructions each are about
+// 1300 of the 2900 cycles that the two streams' softmax takes anyway, on warps of their own.  Warp roles:
+//   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
+//   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q, asks for the codes (L2)
+//   warp 9           issues the tcgen05.mma
+//   warps 12-15      widen K and V
+// The work is cut into equal stretches of tiles, one per SM (rf_cache_attn.cuh); cut items are joined by a second kernel.
+#include <algorithm>
+
+#include "rf_attn_softmax.cuh"
+#include "rf_cache_attn.cuh"
+
+namespace {
+
+using namespace sm100;
+using namespace rf_attn;
+using rf_cache_attn::CacheItem;
+using rf_cache_attn::Stretch;
+using rf_cache_attn::StretchScratch;
+using rf_cache_attn::head_floats;
+using rf_cache_attn::kHeadWords;
+using rf_cache_attn::kOne2;
+using rf_cache_attn::mul_bf16x2;
+using rf_cache_attn::places;
+using rf_cache_attn::widen_even;
+using rf_cache_attn::widen_odd;
+
+constexpr int kRows = 2 * BM, kThreads = 512;
+constexpr int kPagesWarp = 8, kMmaWarp = 9, kWidenWarp = 12;
+constexpr int kItemSlots = 2, kItemWords = 16, kItemReaders = 8;   // readers: the softmax warps
+constexpr int kRecords = 8, kBatch = 8;
+constexpr uint32_t kMore = 4, kLast = 8;
+enum { kHeadPiece = 1, kTailPiece = 2 };
+// Register split: 2 x 128 softmax threads, 128 of the pages / MMA warpgroup, 128 that widen.  Checked like the clip kernel's
+// (see rf_regs_ok): against the register file here, against what the launch really owns on the host.
+constexpr int kRegsSoftmax = 200, kRegsControl = 48, kRegsWiden = 64;
+static_assert(256 * kRegsSoftmax + 128 * kRegsControl + 128 * kRegsWiden <= 65536, "setmaxnreg split exceeds the register file of an SM");
+#define RF_REGS_SOFTMAX() asm volatile("setmaxnreg.inc.sync.aligned.u32 200;")
+#define RF_REGS_CONTROL() asm volatile("setmaxnreg.dec.sync.aligned.u32 48;")
+#define RF_REGS_WIDEN() asm volatile("setmaxnreg.dec.sync.aligned.u32 64;")
+static_assert(kRegsSoftmax == 200 && kRegsControl == 48 && kRegsWiden == 64, "keep the macros in step");
+
+constexpr float kLazyRaise = 32.0f;                         // as in the clip kernel: see there
+constexpr float kRaise = 25.0f, kRaiseMargin = 8.0f;
+constexpr int kSpec = 32;
+
+// Shared memory, TMEM columns and operand layouts are those of the clip kernel (rf_attn.cu: Cfg), where they are explained: K and Q in
+// blocks of 64 columns with 128-byte swizzle, V in blocks of VBOX columns with a block of ones behind them whose product is
+// the row sum of the rounded weights, P on top of S (D = 96 / 128) or in columns of its own (D = 64).
+template <int D>
+struct Cfg {
+  static constexpr int KB = (D + 63) / 64;
+  static constexpr uint32_t BLK = 128 * 128, TILE = KB * BLK;
+  static constexpr bool S_EARLY = D == 64;
+  static constexpr int NK = D == 64 ? 3 : 2, NV = NK;
+  static __host__ __device__ constexpr uint32_t koff(int ks) { return ks < 4 ? (uint32_t)ks * 32u : BLK + (uint32_t)(ks - 4) * 32u; }
+  static constexpr int VBOX = D == 96 ? 32 : 64;
+  static constexpr uint32_t VROW = VBOX * 2, VBLK = 128 * VROW, VLOAD = D / VBOX * VBLK, VTILE = VLOAD + VBLK;
+  static constexpr int NPV = D + 16;
+  static constexpr int PARTS = D == 64 ? 1 : 2;
+  static __host__ __device__ constexpr int cut(int p) { return p * (BN / PARTS); }
+  static __host__ __device__ constexpr uint32_t vchunk(int row, int c) { return row * VROW + ((VBOX == 64 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4); }
+  static __host__ __device__ constexpr uint32_t kchunk(int row, int c) { return (c >> 3) * BLK + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
+  static constexpr uint32_t Q = 0, K0 = 2 * TILE, V0 = K0 + NK * TILE, BAR = V0 + NV * VTILE;
+  static constexpr int B_Q = 0, B_QE = 1, B_KF = 2, B_KE = B_KF + NK, B_VF = B_KE + NK, B_VE = B_VF + NV, B_SF = B_VE + NV, B_PF = B_SF + 2,
+                       B_OF = B_PF + 2 * PARTS, B_SE = B_OF + 2, B_IF = B_SE + 2, B_IE = B_IF + kItemSlots, B_RF = B_IE + kItemSlots,
+                       B_RE = B_RF + kRecords, B_COUNT = B_RE + kRecords;
+  static constexpr uint32_t MISC = BAR + 8 * B_COUNT;
+  static constexpr uint32_t ITEM = (MISC + 16 + 15) / 16 * 16;
+  static constexpr uint32_t RECORD = ITEM + kItemSlots * kItemWords * 4;    // kRecords of 8 words
+  static constexpr uint32_t FLAGS = RECORD + kRecords * 32;                 // a tile's flags for the MMA thread, by K slot
+  static constexpr uint32_t WINDOW = FLAGS + 16;                            // kBatch entries of the two lists, then a batch of the union
+  static constexpr uint32_t SCRATCH = WINDOW + 4 * kBatch * 4;
+  static constexpr uint32_t TOTAL = SCRATCH + sizeof(StretchScratch);
+  static constexpr uint32_t ALLOC = TOTAL + 1024;
+  static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
+  static constexpr bool S_SHARED = D != 96;
+  static constexpr uint32_t S_COL0 = 0, S_COL1 = S_SHARED ? 96 : 128, S_END = S_COL1 + 128, TMEM_COLS = 512;
+  static constexpr uint32_t P_COL0 = S_EARLY ? S_END : S_COL0, P_COL1 = S_EARLY ? S_END + 64 : S_COL1 + 64;
+  static constexpr uint32_t O_COL0 = S_EARLY ? S_END + 128 : S_END, O_COL1 = O_COL0 + NPV;
+  static_assert(O_COL1 + NPV <= TMEM_COLS, "TMEM columns");
+  static constexpr size_t PIECE = (size_t)(D / 4 + 1) * BM;                 // float4 of one piece of one stream: O, then {m, l, l exact, has O}
+};
+
+// The two streams' lists of an item: how long they are and how many places of the line the item takes.
+struct Streams { int n0, n1, sees0, sees1; };
+__device__ __forceinline__ Streams streams(const RfCacheAttn& a, const CacheItem& it) {
+  Streams s;
+  const int tile = it.r0 / kPage;
+  s.sees0 = rf_rows_see(a.u, it.len, it.q_len, it.r0, BM);
+  s.sees1 = it.r0 + BM < a.u.rows ? rf_rows_see(a.u, it.len, it.q_len, it.r0 + BM, BM) : -1;
+  if (a.count == nullptr) {
+    s.n0 = rf_pages(max(s.sees0, 0));
+    s.n1 = rf_pages(max(s.sees1, 0));
+  } else {
+    s.n0 = s.sees0 < 0 ? 0 : rf_cache_attn::listed(a, it, tile);
+    s.n1 = s.sees1 < 0 ? 0 : rf_cache_attn::listed(a, it, tile + 1);
+  }
+  return s;
+}
+struct ChunkPlaces {
+  static constexpr int kRowsOf = kRows;
+  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+    const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
+    if (it.sees < 0) return 0;
+    const Streams s = streams(a, it);
+    return places(max(s.n0, s.n1));
+  }
+};
+
+struct Item { int bh, r0, len, q_len, pages, n0, n1, b0, b1, cut; };
+
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// Which 16-byte chunk of codes a thread of the widening warps takes in pass p: eight neighbouring lanes write eight
+// different 16-byte columns of shared memory (nearly so at D = 96).
+template <int D>
+__device__ __forceinline__ void widen_place(int p, int warp, int lane, int& row, int& c) {
+  if (D == 128) {
+    row = p * 16 + warp * 4 + ((lane >> 4) & 1) * 2 + ((lane >> 2) & 1);
+    c = ((lane >> 3) & 1) * 4 + (lane & 3);
+  } else if (D == 64 || p < 4) {
+    row = p * 32 + warp * 8 + (lane >> 2);
+    c = lane & 3;
+  } else {
+    row = (p - 4) * 64 + warp * 16 + (lane >> 1);
+    c = 4 + (lane & 1);
+  }
+}
+
+struct Maps { CUtensorMap q; };
+
+template <int D, bool LSE>
+__global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
+  using C = Cfg<D>;
+  constexpr uint32_t IDESC_S = idesc_bf16(BM, BN, 0), IDESC_PV = idesc_bf16(BM, C::NPV, 1);
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  auto bar = [&](int slot) -> uint32_t { return base + C::BAR + 8u * slot; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(base_ptr + C::MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC + 8);
+  int* items = reinterpret_cast<int*>(base_ptr + C::ITEM);
+  volatile uint32_t* records = reinterpret_cast<volatile uint32_t*>(base_ptr + C::RECORD);
+  volatile uint32_t* flags = reinterpret_cast<volatile uint32_t*>(base_ptr + C::FLAGS);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    mbar_init(bar(C::B_Q), 1);
+    mbar_init(bar(C::B_QE), 1);
+    for (int s = 0; s < C::NK; ++s) {
+      mbar_init(bar(C::B_KF + s), 4); mbar_init(bar(C::B_KE + s), 1);
+      mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1);
+    }
+    for (int j = 0; j < 2; ++j) {
+      mbar_init(bar(C::B_SF + j), 1);
+      for (int p = 0; p < C::PARTS; ++p) mbar_init(bar(C::B_PF + j * C::PARTS + p), 4);
+      mbar_init(bar(C::B_OF + j), 1);
+      mbar_init(bar(C::B_SE + j), 4);
+    }
+    for (int i = 0; i < kItemSlots; ++i) { mbar_init(bar(C::B_IF + i), 1); mbar_init(bar(C::B_IE + i), kItemReaders); }
+    for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::B_RF + i), 1); mbar_init(bar(C::B_RE + i), 4); }
+    *abort_flag = 0;
+    mbar_init_fence();
+  }
+  for (int i = tid; i < C::NV * BN * 2; i += kThreads) {   // the 16 columns behind V's: one, then zeros
+    const int v = i / (BN * 2), row = i / 2 % BN, c = i % 2;
+    *reinterpret_cast<uint4*>(base_ptr + C::V0 + v * C::VTILE + C::VLOAD + C::vchunk(row, c)) = make_uint4(c == 0 ? 0x3f80u : 0u, 0u, 0u, 0u);
+  }
+  fence_proxy_async_smem();
+  if (warp == kPagesWarp) {
+    if (lane == 0) prefetch_tmap(&maps.q);
+    __syncwarp();
+    tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
+  }
+  rf_grid_trigger();
+  rf_grid_wait();
+  tc_fence_before();
+  const Stretch st = rf_cache_attn::stretch<ChunkPlaces, kThreads>(a, reinterpret_cast<StretchScratch*>(base_ptr + C::SCRATCH));   // (has barriers)
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const WaitCtx wc{abort_flag, a.dev_status};
+  if (tid == 0) {
+    int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
+    head[0] = st.item;
+    head[3] = st.lo < st.hi && st.at < st.lo;
+  }
+
+  if (warp >= kWidenWarp) {
+    RF_REGS_WIDEN();
+    // ------------------------------------------------------------ codes to bf16
+    constexpr int kPasses = D / 16;
+    const int w = warp - kWidenWarp;
+    uint4 x[kPasses];
+    auto load = [&](const uint8_t* codes, uint32_t row_of_pages) {
+      const uint8_t* src = codes + (size_t)row_of_pages * (kPage * D);
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        int row, c;
+        widen_place<D>(p, w, lane, row, c);
+        x[p] = *reinterpret_cast<const uint4*>(src + row * D + c * 16);
+      }
+    };
+    auto store = [&](bool keys, uint32_t to, uint32_t m1, uint32_t m2) {
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        int row, c;
+        widen_place<D>(p, w, lane, row, c);
+        uint32_t y[8];
+        const uint32_t* in = &x[p].x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t t = __byte_perm(in[i], 0u, 0x3120);       // bytes 0 1 | 2 3 to where widen_even and widen_odd look
+          y[2 * i] = mul_bf16x2(widen_even(t), m1);
+          y[2 * i + 1] = mul_bf16x2(widen_odd(t), m1);
+        }
+        if (m2 != kOne2) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = mul_bf16x2(y[i], m2);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t at;
+          if (keys) at = to + C::kchunk(row, 2 * c + i);
+          else at = to + (2 * c / (C::VBOX / 8)) * C::VBLK + C::vchunk(row, (2 * c + i) % (C::VBOX / 8));
+          sts128(at, y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    bool ok = true;
+    for (int u = 0;; ++u) {
+      const int slot = u % kRecords, ks = u % C::NK;
+      ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RF + slot), (u / kRecords) & 1, wc, 0));
+      if (!ok) break;
+      volatile const uint32_t* r = records + slot * 8;
+      const uint32_t f = r[0], row = r[1], k1 = r[2], k2 = r[3], v1 = r[4], v2 = r[5];
+      if (f & kMore) load(a.c.k, row);
+      if (u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc));
+      if (!ok) break;
+      if (f & kMore) store(true, base + C::K0 + ks * C::TILE, k1, k2);
+      if (w == 0 && lane == 0) flags[ks] = f;
+      if (lane == 0) mbar_arrive(bar(C::B_KF + ks));
+      if (!(f & kMore)) break;
+      load(a.c.v, row);
+      if (lane == 0) mbar_arrive(bar(C::B_RE + slot));
+      if (u >= C::NV) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_VE + ks), ((u / C::NV) - 1) & 1, wc));
+      if (!ok) break;
+      store(false, base + C::V0 + ks * C::VTILE, v1, v2);
+      if (lane == 0) mbar_arrive(bar(C::B_VF + ks));
+    }
+  } else if (warp >= kPagesWarp) {
+    RF_REGS_CONTROL();
+    if (warp == kPagesWarp) {
+      // ------------------------------------------------------------ pages
+      int* win = reinterpret_cast<int*>(base_ptr + C::WINDOW);
+      int no = 0, u = 0, nq = 0;          // items published, tiles published, Q fetched
+      long long at = st.at;
+      int item = st.item;
+      bool ok = true;
+      for (long long pos = st.lo; pos < st.hi && ok; ++item) {
+        const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
+        if (it.sees < 0) continue;
+        const Streams s = streams(a, it);
+        const int n = places(max(s.n0, s.n1)), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+        int b0, b1, e0, e1;
+        if (a.count == nullptr) {       // the streams keep step: they share their tiles
+          b0 = min(begin, s.n0); e0 = min(end, s.n0);
+          b1 = min(begin, s.n1); e1 = min(end, s.n1);
+        } else {
+          b0 = (int)((long long)s.n0 * begin / n); e0 = (int)((long long)s.n0 * end / n);
+          b1 = (int)((long long)s.n1 * begin / n); e1 = (int)((long long)s.n1 * end / n);
+        }
+        const int pages = rf_pages(it.len), slot = no % kItemSlots;
+        if (no >= kItemSlots) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_IE + slot), ((no / kItemSlots) - 1) & 1, wc, end - begin));
+        if (!ok) break;
+        if (lane == 0) {
+          int* w = items + slot * kItemWords;
+          w[0] = it.bh; w[1] = it.r0; w[2] = it.len; w[3] = it.q_len; w[4] = pages; w[5] = e0 - b0; w[6] = e1 - b1; w[7] = b0; w[8] = b1;
+          w[9] = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
+          mbar_arrive(bar(C::B_IF + slot));
+        }
+        ++no;
+        at += n;
+        pos = at;
+        if (e0 == b0 && e1 == b1) continue;                    // sees nothing, or lists nothing here
+        if (nq > 0) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QE), (nq - 1) & 1, wc, end - begin));
+        if (!ok) break;
+        if (lane == 0) {
+          mbar_expect_tx(bar(C::B_Q), 2 * C::TILE);
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int kb = 0; kb < C::KB; ++kb)
+              tma_load_3d(base + C::Q + j * C::TILE + kb * C::BLK, &maps.q, kb * 64, it.r0 + j * BM, it.bh, bar(C::B_Q));
+        }
+        ++nq;
+        const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
+        const int32_t* l1 = l0 != nullptr && it.r0 / kPage + 1 < a.u.n_q ? l0 + a.n_k : l0;
+        int i0 = b0, i1 = b1;
+        while ((i0 < e0 || i1 < e1) && ok) {
+          // a batch of the union: entries past the sequence count as page `pages`, which no row sees
+          int m0 = 0x7fffffff, m1 = 0x7fffffff;
+          if (lane < kBatch) {
+            if (i0 + lane < e0) m0 = l0 != nullptr ? l0[i0 + lane] : i0 + lane;
+            if (i1 + lane < e1) m1 = l1 != nullptr ? l1[i1 + lane] : i1 + lane;
+            if (i0 + lane < e0 && (m0 < 0 || m0 >= pages)) { m0 = pages; rf_report(a.dev_status, RF_ERR_INVALID_ARG); }
+            if (i1 + lane < e1 && (m1 < 0 || m1 >= pages)) { m1 = pages; rf_report(a.dev_status, RF_ERR_INVALID_ARG); }
+            win[lane] = m0;
+            win[kBatch + lane] = m1;
+          }
+          __syncwarp();
+          int take0 = 0, take1 = 0, cnt = 0;
+          if (lane == 0) {
+            for (; cnt < kBatch; ++cnt) {
+              const int h0 = take0 < kBatch ? win[take0] : 0x7fffffff, h1 = take1 < kBatch ? win[kBatch + take1] : 0x7fffffff;
+              const int h = min(h0, h1);
+              if (h == 0x7fffffff) break;
+              win[2 * kBatch + cnt] = h;
+              win[3 * kBatch + cnt] = (h0 == h ? 1 : 0) | (h1 == h ? 2 : 0);
+              take0 += h0 == h;
+              take1 += h1 == h;
+            }
+          }
+          __syncwarp();
+          take0 = __shfl_sync(0xffffffffu, take0, 0);
+          take1 = __shfl_sync(0xffffffffu, take1, 0);
+          cnt = __shfl_sync(0xffffffffu, cnt, 0);
+          i0 += take0;
+          i1 += take1;
+          uint32_t row = 0, f = 0;
+          rf_cache_attn::Widen kw = {kOne2, kOne2}, vw = kw;
+          if (lane < cnt) {
+            const int page = win[2 * kBatch + lane];
+            f = (uint32_t)win[3 * kBatch + lane] | kMore;
+            if (lane == cnt - 1 && i0 == e0 && i1 == e1) f |= kLast;
+            const int phys = rf_page(a.c, it.b, min(page, pages - 1), a.dev_status);   // (a page that no row sees: any will do)
+            row = (uint32_t)phys * a.c.H + it.bh % a.c.H;
+            prefetch_l2(a.c.k + (size_t)row * (kPage * D), kPage * D);
+            prefetch_l2(a.c.v + (size_t)row * (kPage * D), kPage * D);
+            kw = rf_cache_attn::widen_by(a.c.k_scale[row]);
+            vw = rf_cache_attn::widen_by(a.c.v_scale[row]);
+          }
+          // the records' slots one after the other, each filled by the lane that looked it up
+          for (int i = 0; i < cnt && ok; ++i, ++u) {
+            const int rs = u % kRecords;
+            if (u >= kRecords) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0));
+            if (ok && lane == i) {
+              volatile uint32_t* r = records + rs * 8;
+              r[0] = f; r[1] = row; r[2] = kw.m1; r[3] = kw.m2; r[4] = vw.m1; r[5] = vw.m2;
+              mbar_arrive(bar(C::B_RF + rs));
+            }
+          }
+          __syncwarp();
+        }
+      }
+      // the end, for the warps that walk tiles and for those that walk items
+      const int rs = u % kRecords, slot = no % kItemSlots;
+      if (u >= kRecords) mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0);
+      if (no >= kItemSlots) mbar_wait_long(bar(C::B_IE + slot), ((no / kItemSlots) - 1) & 1, wc, (int)min(st.hi - st.lo, 1ll << 20));
+      if (lane == 0) {
+        records[rs * 8] = 0;
+        mbar_arrive(bar(C::B_RF + rs));
+        items[slot * kItemWords] = -1;
+        mbar_arrive(bar(C::B_IF + slot));
+      }
+    } else if (warp == kMmaWarp) {
+      // ------------------------------------------------------------ MMA issuer
+      if (C::S_EARLY ? lane == 0 : elect_one()) {
+        constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+        constexpr uint32_t DESC_HI_V = C::VBOX == 64 ? DESC_HI : (512u >> 4) | (1u << 14) | (4u << 29);
+        constexpr uint32_t LO_KMAJOR = 1u << 16, LO_VMAJOR = (C::VBLK >> 4) << 16;
+        auto desc = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI << 32) | lo; };
+        auto desc_v = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI_V << 32) | lo; };
+        const uint32_t q_lo = ((base + C::Q) >> 4) | LO_KMAJOR, k_lo = ((base + C::K0) >> 4) | LO_KMAJOR;
+        const uint32_t v_lo = ((base + C::V0) >> 4) | LO_VMAJOR;
+        auto issue_s = [&](int j, int ks) {
+          uint32_t a0 = q_lo + j * (C::TILE >> 4);
+          const uint32_t b0 = k_lo + ks * (C::TILE >> 4);
+          asm volatile("" : "+r"(a0));
+          const uint32_t t_d = tmem_base + (j ? C::S_COL1 : C::S_COL0);
+          mma_ss_c<false>(t_d, desc(a0), desc(b0), IDESC_S);
+#pragma unroll
+          for (int k = 1; k < D / 16; ++k) mma_ss_c<true>(t_d, desc(a0 + (C::koff(k) >> 4)), desc(b0 + (C::koff(k) >> 4)), IDESC_S);
+          tc_commit(bar(C::B_SF + j));
+        };
+        auto issue_pv = [&](int j, int vs, uint32_t acc, uint32_t par) {
+          const uint32_t b0 = v_lo + vs * (C::VTILE >> 4);
+          const uint32_t t_p = tmem_base + (j ? C::P_COL1 : C::P_COL0), t_o = tmem_base + (j ? C::O_COL1 : C::O_COL0);
+#pragma unroll
+          for (int p = 0; p < C::PARTS; ++p) {
+            mbar_wait(bar(C::B_PF + j * C::PARTS + p), par, wc);
+            tc_fence_after();
+#pragma unroll
+            for (int k = C::cut(p) / 16; k < C::cut(p + 1) / 16; ++k) {
+              if (k == 0) mma_ts(t_o, t_p, desc_v(b0), IDESC_PV, acc);
+              else mma_ts_c<true>(t_o, t_p + k * 8, desc_v(b0 + k * (16 * C::VROW >> 4)), IDESC_PV);
+            }
+          }
+          tc_commit(bar(C::B_OF + j));
+        };
+        uint32_t pv_par = 0, s_par = 3, acc = 0, nq = 0, cur = 0;
+        auto s_free = [&](int j) {
+          if (C::S_EARLY) mbar_wait(bar(C::B_SE + j), (s_par >> j) & 1, wc);
+          if (C::S_SHARED) mbar_wait(bar(C::B_SE + (j ^ 1)), (s_par >> (j ^ 1)) & 1, wc);
+          if (C::S_EARLY || C::S_SHARED) tc_fence_after();
+          s_par ^= 1u << j;
+        };
+        // the next tile's flags, once its K is in place; nothing after an abandoned wait
+        auto next = [&](int u) -> uint32_t {
+          if (!mbar_wait_long(bar(C::B_KF + u % C::NK), (u / C::NK) & 1, wc, 0)) return 0u;
+          tc_fence_after();
+          return flags[u % C::NK];
+        };
+        // the scores of an item's first tile, for both streams
+        auto open = [&](uint32_t rec, int u) {
+          mbar_wait(bar(C::B_Q), nq & 1, wc);
+          ++nq;
+          tc_fence_after();
+#pragma unroll 1
+          for (int j = 0; j < 2; ++j)
+            if (rec & (1 << j)) { s_free(j); issue_s(j, u % C::NK); }
+          tc_commit(bar(C::B_KE + u % C::NK));
+          if (rec & kLast) tc_commit(bar(C::B_QE));
+        };
+        cur = next(0);
+        if (cur & kMore) open(cur, 0);
+        for (int u = 0; cur & kMore; ++u) {
+          const int vs = u % C::NV, ks = (u + 1) % C::NK;
+          uint32_t nxt = 0;
+          if (cur & kLast) {
+            if (!mbar_wait(bar(C::B_VF + vs), (u / C::NV) & 1, wc)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int j = 0; j < 2; ++j) {
+              if (cur & (1 << j)) {
+                issue_pv(j, vs, (acc >> j) & 1, (pv_par >> j) & 1);
+                pv_par ^= 1u << j;
+              }
+            }
+            tc_commit(bar(C::B_VE + vs));
+            acc = 0;
+            nxt = next(u + 1);
+            if (nxt & kMore) open(nxt, u + 1);
+          } else {
+            nxt = next(u + 1);
+            if (!(nxt & kMore)) break;
+            if (!mbar_wait(bar(C::B_VF + vs), (u / C::NV) & 1, wc)) break;
+            tc_fence_after();
+            if constexpr (C::S_EARLY) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks); }
+                if (cur & (1 << j)) {
+                  issue_pv(j, vs, (acc >> j) & 1, (pv_par >> j) & 1);
+                  acc |= 1u << j;
+                  pv_par ^= 1u << j;
+                }
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                if (cur & (1 << j)) {
+                  issue_pv(j, vs, (acc >> j) & 1, (pv_par >> j) & 1);
+                  acc |= 1u << j;
+                  pv_par ^= 1u << j;
+                }
+                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks); }
+              }
+            }
+            tc_commit(bar(C::B_KE + ks));
+            tc_commit(bar(C::B_VE + vs));
+            if (nxt & kLast) tc_commit(bar(C::B_QE));
+          }
+          cur = nxt;
+        }
+      }
+    }
+  } else {
+    RF_REGS_SOFTMAX();
+    // ------------------------------------------------------------ softmax + epilogue, one thread per query row (as in the clip kernel)
+    const int j = warp >> 2, row_in_tile = tid & 127;
+    const uint32_t lane_sel = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem_base + lane_sel + (j ? C::S_COL1 : C::S_COL0);
+    const uint32_t t_o = tmem_base + lane_sel + (j ? C::O_COL1 : C::O_COL0);
+    const float sc = a.scale_log2;
+    uint32_t done = 0;
+    int waited = 0;
+    for (int item = 0;; ++item) {
+      const int slot = item % kItemSlots;
+      const int* iw = items + slot * kItemWords;
+      if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_IF + slot), (item / kItemSlots) & 1, wc, waited))) break;
+      if (iw[0] < 0) break;
+      const int n = iw[5 + j], begin = iw[7 + j], end = begin + n, pages = iw[4];
+      waited = iw[5] + iw[6];
+      const int r = iw[1] + j * BM + row_in_tile;
+      int sees = 0;                                       // keys that this row sees; none if it is padding
+      if (r < a.u.rows && r % a.u.M < iw[3]) sees = rf_row_sees(a.u.causal, iw[2], iw[3], r % a.u.M);
+      const int32_t* list = a.count != nullptr ? a.pages + ((size_t)iw[0] * a.u.n_q + min(iw[1] / kPage + j, a.u.n_q - 1)) * a.n_k : nullptr;
+      float m_run = -INFINITY, l_run = 0.f, l_exact = 0.f;
+      bool opens = true;
+      for (int t = begin; t < end; ++t, ++done, opens = false) {
+        int page = list != nullptr ? list[t] : t;
+        if (page < 0 || page >= pages) page = pages;
+        const int left = sees - page * kPage;             // keys of the tile that this row sees (page <= 2^23: no overflow)
+        const bool partial = __any_sync(0xffffffffu, left < BN);
+        mbar_wait(bar(C::B_SF + j), done & 1, wc);
+        tc_fence_after();
+        uint32_t s[128];
+        uint32_t l_tile;
+        if constexpr (!C::S_EARLY) l_tile = tmem_ld1(t_o + D);
+        load_scores(t_s, s);
+        if constexpr (!C::S_EARLY) l_run = opens ? 0.f : l_run + __uint_as_float(l_tile);
+        if constexpr (C::S_SHARED) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::B_SE + j));
+        }
+        if (partial) {
+#pragma unroll
+          for (int c = 0; c < BN; ++c)
+            if (c >= left) s[c] = 0xff800000u;
+        }
+        if constexpr (C::S_EARLY) {
+          float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 128; c += 4) {
+            mx0 = fmaxf(mx0, fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+            mx1 = fmaxf(mx1, fmaxf(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])));
+          }
+          const float m_tile = fmaxf(mx0, mx1) * sc;
+          const bool raise = m_tile > m_run + kLazyRaise || (m_run == -INFINITY && m_tile > -INFINITY);
+          const bool any_raise = __any_sync(0xffffffffu, raise);
+          float alpha = 1.f;
+          if (raise) {
+            alpha = ex2(m_run - m_tile);
+            m_run = m_tile;
+            l_run *= alpha;
+            if (LSE) l_exact *= alpha;
+          }
+          bool o_landed = opens;
+          if (!opens && any_raise) {
+            mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
+            o_landed = true;
+            rescale_o<D>(t_o, alpha);
+          }
+          const float m_use = m_run == -INFINITY ? 0.f : m_run;
+          const float2 sc2 = make_float2(sc, sc), mneg = make_float2(-m_use, -m_use);
+          float2 la = make_float2(0.f, 0.f);
+          uint32_t pk[64];
+          take_weights<0, BN, LSE>(s, pk, la, sc2, mneg);
+          if (LSE) l_exact += la.x + la.y;
+          if (!o_landed) mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
+          tc_fence_after();
+          l_tile = tmem_ld1(t_o + D);
+          {
+            const uint32_t t_p = tmem_base + lane_sel + (j ? C::P_COL1 : C::P_COL0);
+            uint32_t(&p0)[32] = *reinterpret_cast<uint32_t(*)[32]>(&pk[0]);
+            uint32_t(&p1)[32] = *reinterpret_cast<uint32_t(*)[32]>(&pk[32]);
+            tmem_st32(t_p, p0);
+            tmem_st32(t_p + 32, p1);
+            tc_wait_ld();
+            tmem_st1(t_o + D, 0u);
+            tc_wait_st();
+          }
+          l_run = opens ? 0.f : l_run + __uint_as_float(l_tile) * alpha;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::B_PF + j));
+          continue;
+        }
+        uint32_t pk[64];
+        float2 la = make_float2(0.f, 0.f);
+        const float2 sc2 = make_float2(sc, sc);
+        float m_use = m_run == -INFINITY ? 0.f : m_run;
+        take_weights<0, kSpec, LSE>(s, pk, la, sc2, make_float2(-m_use, -m_use));
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 128; c += 4) {
+          mx0 = fmaxf(mx0, fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+          mx1 = fmaxf(mx1, fmaxf(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])));
+        }
+        const float m_tile = fmaxf(mx0, mx1) * sc;
+        if (__any_sync(0xffffffffu, m_tile > m_run + kRaise)) {
+          float alpha = 1.f;
+          if (m_tile > m_run + kRaiseMargin) {
+            alpha = ex2(m_run - m_tile);
+            m_run = m_tile;
+            l_run *= alpha;
+            if (LSE) l_exact *= alpha;
+          }
+          if (!opens) {
+            mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
+            rescale_o_call<D>(t_o, alpha);
+          }
+          m_use = m_run == -INFINITY ? 0.f : m_run;
+          la = make_float2(0.f, 0.f);
+          take_weights<0, kSpec, LSE>(s, pk, la, sc2, make_float2(-m_use, -m_use));
+        }
+        const uint32_t t_p = tmem_base + lane_sel + (j ? C::P_COL1 : C::P_COL0);
+        const float2 mneg = make_float2(-m_use, -m_use);
+        take_weights<kSpec, 64, LSE>(s, pk, la, sc2, mneg);
+        store_weights<0, 64>(t_p, pk);
+        tmem_st1(t_o + D, 0u);
+        take_weights<64, 80, LSE>(s, pk, la, sc2, mneg);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::B_PF + j * C::PARTS));
+        take_weights<80, BN, LSE>(s, pk, la, sc2, mneg);
+        store_weights<64, BN>(t_p, pk);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::B_PF + j * C::PARTS + 1));
+        if (LSE) l_exact += la.x + la.y;
+      }
+      if (n > 0) {
+        mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
+        tc_fence_after();
+        const uint32_t l_tile = tmem_ld1(t_o + D);
+        tc_wait_ld();
+        l_run += __uint_as_float(l_tile);
+      }
+      const int cut = iw[9];
+      if (cut) {
+        float4* mine = reinterpret_cast<float4*>(a.ws + head_floats(gridDim.x)) +
+                       (((size_t)2 * blockIdx.x + (cut & kTailPiece ? 1 : 0)) * 2 + j) * C::PIECE + row_in_tile;
+        if (n > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t v[32];
+            tmem_ld32(t_o + c * 32, v);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              __stcg(mine + (c * 8 + i) * BM, make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
+                                                          __uint_as_float(v[4 * i + 3])));
+          }
+        }
+        __stcg(mine + (D / 4) * BM, make_float4(m_run, l_run, l_exact, n > 0 ? 1.f : 0.f));
+      } else {
+        const bool there = r < a.u.rows && r % a.u.M < iw[3];
+        const size_t at_row = (size_t)iw[0] * a.u.rows + min(r, a.u.rows - 1);
+        uint4* o = reinterpret_cast<uint4*>(a.o + at_row * D);
+        const bool o32 = (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0;
+        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          if (n > 0) {                                     // (the same for the whole warp)
+            tmem_ld32(t_o + c * 32, v);
+            tc_wait_ld();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0u;
+          }
+          if (there) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+            store_columns(o + c * 4, v, o32);
+          }
+        }
+        if (LSE && there) a.lse[at_row] = (m_run + log2f(l_exact)) * 0.6931471805599453f;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::B_IE + slot));
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kPagesWarp) {
+    if (*abort_flag) __nanosleep(20000);
+    __syncwarp();
+    tmem_dealloc(tmem_base, C::TMEM_COLS);
+  }
+}
+
+// Joins the pieces of the items that the stretches cut (see rf_cache_join_kernel): a thread per row, blockIdx.y = stream and 16 columns.
+template <int D, bool LSE>
+__global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_constant__ RfCacheAttn a, int ctas) {
+  using C = Cfg<D>;
+  rf_grid_trigger();
+  rf_grid_wait();
+  const int x = blockIdx.x + 1, j = blockIdx.y / (D / 16), c0 = blockIdx.y % (D / 16) * 4;
+  const int32_t* heads = reinterpret_cast<const int32_t*>(a.ws);
+  const int32_t* mine = heads + x * kHeadWords;
+  if (!mine[3]) return;
+  if (mine[3 - kHeadWords] && mine[-kHeadWords] == mine[0]) return;
+  int n = 1;
+  while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
+  const CacheItem it = rf_cache_attn::cache_item<kRows>(a, mine[0]);
+  const int row = it.r0 + j * BM + threadIdx.x;
+  if (row >= a.u.rows || row % a.u.M >= it.q_len) return;
+  const float4* pieces = reinterpret_cast<const float4*>(a.ws + head_floats(ctas)) + threadIdx.x;
+  float m = -INFINITY, l = 0.f, lx = 0.f;
+  float4 acc[4] = {};
+  for (int i = 0; i <= n; ++i) {
+    const float4* at = pieces + ((i == 0 ? (size_t)2 * (x - 1) + 1 : (size_t)2 * (x + i - 1)) * 2 + j) * C::PIECE;
+    const float4 st = __ldcg(at + (D / 4) * BM);
+    if (st.w == 0.f) continue;                          // walked no tile: its O was never written
+    float4 o[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = __ldcg(at + (c0 + k) * BM);
+    float keep = 1.f, w = 1.f;
+    if (st.x > m) {
+      if (m > -INFINITY) keep = ex2(m - st.x);
+      m = st.x;
+    } else if (st.x > -INFINITY) {
+      w = ex2(st.x - m);
+    }
+    l = l * keep + st.y * w;
+    lx = lx * keep + st.z * w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      acc[k].x = acc[k].x * keep + o[k].x * w;
+      acc[k].y = acc[k].y * keep + o[k].y * w;
+      acc[k].z = acc[k].z * keep + o[k].z * w;
+      acc[k].w = acc[k].w * keep + o[k].w * w;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint32_t v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = pack_bf16(acc[k].x * inv, acc[k].y * inv);
+    v[2 * k + 1] = pack_bf16(acc[k].z * inv, acc[k].w * inv);
+  }
+  const size_t at_row = (size_t)it.bh * a.u.rows + row;
+  store_sector(reinterpret_cast<uint4*>(a.o + at_row * D) + c0 / 2, v, (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0);
+  if (LSE && c0 == 0) a.lse[at_row] = (m + log2f(lx)) * 0.6931471805599453f;
+}
+
+int chunk_ctas(const RfCache& c, const RfQueries& u) {
+  const long long items = (long long)c.B * c.H * rf_cdiv(u.rows, kRows), most = items * c.max_pages;
+  return (int)std::min<long long>(most, 148);
+}
+
+template <int D, bool LSE>
+rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
+  using C = Cfg<D>;
+  static bool configured[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return RF_ERR_CUDA;
+  if (dev >= 0 && dev < 64 && !configured[dev]) {
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, rf_cache_chunk_kernel<D, LSE>) != cudaSuccess) return RF_ERR_CUDA;
+    // setmaxnreg.inc draws on what the launch owns: with less it would never be granted
+    if (fa.numRegs * kThreads < 256 * kRegsSoftmax + 128 * kRegsControl + 128 * kRegsWiden) return RF_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(rf_cache_chunk_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::ALLOC) != cudaSuccess)
+      return RF_ERR_CUDA;
+    configured[dev] = true;
+  }
+  Maps maps;
+  if (!rf_encode_rows_map(&maps.q, a.u.q, D, a.u.rows, (size_t)D * 2, (size_t)a.u.rows * D * 2, a.c.B * a.c.H)) return RF_ERR_CUDA;
+  const int ctas = chunk_ctas(a.c, a.u);
+  if (rf_launch(rf_cache_chunk_kernel<D, LSE>, dim3(ctas), kThreads, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
+  if (ctas == 1) return RF_OK;
+  return rf_launch(rf_cache_chunk_join_kernel<D, LSE>, dim3(ctas - 1, 2 * (D / 16)), BM, 0, st, a, ctas) == cudaSuccess ? RF_OK : RF_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t rf_cache_chunk_ws_bytes(const RfCache& c, const RfQueries& u) {
+  const int ctas = chunk_ctas(c, u);
+  return head_floats(ctas) * sizeof(float) + (size_t)2 * ctas * 2 * (c.D / 4 + 1) * BM * sizeof(float4);
+}
+
+rf_status rf_launch_cache_chunk(const RfCacheAttn& a, cudaStream_t st) {
+  const bool lse = a.lse != nullptr;
+  switch (a.c.D) {
+    case 64: return lse ? launch<64, true>(a, st) : launch<64, false>(a, st);
+    case 96: return lse ? launch<96, true>(a, st) : launch<96, false>(a, st);
+    case 128: return lse ? launch<128, true>(a, st) : launch<128, false>(a, st);
+  }
+  return RF_ERR_UNSUPPORTED;
+}

@@ -51,7 +51,7 @@ def test_null_structs():
 
 
 @pytest.mark.parametrize("u,code", [(query(H=0), INVALID), (query(H=7), INVALID), (query(M=0), INVALID), (query(causal=-1), INVALID), (query(scale=float("nan")), INVALID),
-                                    (query(scale=float("inf")), INVALID), (query(H=3, M=(1 << 30) + 1), UNSUPPORTED), (query(H=6, M=1 << 30), UNSUPPORTED)])
+                                    (query(scale=float("inf")), INVALID), (query(scale=-0.1), INVALID), (query(H=3, M=(1 << 30) + 1), UNSUPPORTED), (query(H=6, M=1 << 30), UNSUPPORTED)])
 def test_bad_queries(u, code):
     assert calls(cache(), u=u)[4:] == [code] * 2
     assert api.load().rf_cache_attn_workspace_bytes(C.byref(cache()), C.byref(u)) == 0

@@ -172,7 +172,7 @@ def test_scores_of_every_size(M):
         p.append(k, rng.standard_normal((1, 1, 128, 128)), [128])
     q = rng.standard_normal((1, 1, M, 128)) * 3
     p.attend(q, scale=0.3)
-    p.attend(q, scale=-0.05)
+    p.attend(q, scale=1e-3)
     p.attend(q * 0, scale=1.0)
 
 
