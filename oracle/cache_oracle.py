@@ -168,12 +168,12 @@ class Cache:
         return out
 
     def attend(self, q, q_len, causal=0, scale=None, lists=None):
-        """(o, lse, spread, reach) for q [B, H, M, D], each [B, H, M(, D)]; padding rows are NaN.  spread = sum of weights * |v|,
-        reach = the largest scale * sum |q| |k| of a row: what the error bounds are made of."""
+        """(o, lse, spread, reach, wide) for q [B, H, M, D], each [B, H, M(, D)]; padding rows are NaN.  spread = sum of weights *
+        |v|, reach = the largest scale * sum |q| |k| of a row, wide = scale * max |q| * the largest sum |k|: what the error bounds are made of."""
         B, H, M, D = q.shape
         G, scale = H // self.H, D ** -0.5 if scale is None else scale
         o, spread = np.full((B, H, M, D), np.nan), np.full((B, H, M, D), np.nan)
-        lse, reach = np.full((B, H, M), np.nan), np.full((B, H, M), np.nan)
+        lse, reach, wide = (np.full((B, H, M), np.nan) for _ in range(3))
         for b in range(B):
             m = q_len[b]
             if m == 0:
@@ -200,5 +200,6 @@ class Cache:
                 with np.errstate(divide="ignore"):
                     lse[b, h, :m] = np.log(total) + np.where(np.isfinite(top), top, 0.0)[:, 0]
                 o[b, h, :m], spread[b, h, :m] = w @ v, w @ np.abs(v)
+                wide[b, h, :m] = (np.where(keep, abs(scale) * np.abs(k).sum(1)[None, :], 0.0)).max(1, initial=0.0) * np.abs(x).max(1)
                 reach[b, h, :m] = (np.where(keep, abs(scale) * (np.abs(x) @ np.abs(k).T), 0.0)).max(1, initial=0.0)
-        return o, lse, spread, reach
+        return o, lse, spread, reach, wide

@@ -2,14 +2,23 @@
 //
 // o = softmax(scale q k^T) v over the keys that each row sees.  From some dozens of rows on the products bound it, not the
 // cache's bytes.  An item is 256 query rows of one K/V head in two tiles of 128 (two "streams"), as in the attention
-// kernel over whole clips, whose softmax it shares; what differs is where K and V come from.  They lie in pages, as codes:
-// four warps load a tile's codes, widen them to bf16 (exact, see widen_odd) and lay them out in shared memory in the swizzled
-// form that tcgen05 reads.  A tile of 128 keys is widened once for its 256 rows: 32 768 codes at 2.5 integer instructions each are about
-// 1300 of the 2900 cycles that the two streams' softmax takes anyway, on warps of their own.  Warp roles:
+// kernel over whole clips, whose softmax it shares; what differs is where K and V come from: pages of e4m3 codes.
+//
+// Scores: K's codes go to the tensor cores as they are (kind::f8f6f4), and each query row, which is bf16, as a sum of two 8-bit
+// numbers.  With the row scaled by a power of two to a largest magnitude in (224, 448], hi = e4m3(q) leaves at most 8 units of q's last place, which
+// e5m2 holds exactly: q = hi + lo exactly from 2^-6 up (2^-14 of the row's largest), and below to within 2^-14 (2^-21.8 of the largest, the
+// order of an fp32 sum's own rounding).  hi K^T + lo K^T costs what one bf16 product costs, reads half the shared memory, and nothing has
+// to be widened; the page's scale and the row's go into the softmax's factor.
+// Values: the weights have to be bf16 (they span more binades than 8 bits hold), so V is widened to bf16 (exact, see widen_odd) by four
+// warps, once for the 256 rows, and laid out in shared memory in the swizzled form that tcgen05 reads, beside the softmax.
+// (K widened as well, by the same four warps: 6650 cycles a tile instead of the softmax's 2900, twice 1450 for the two and twice 900
+// for the loads, as shared memory then carries 32 KB more a tile beside the operands' 200; 24 heads, 2040 rows, 32 896 keys, D = 128:
+// 1090 us.)
+// Warp roles:
 //   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
-//   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q, asks for the codes (L2)
+//   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches K by TMA
 //   warp 9           issues the tcgen05.mma
-//   warps 12-15      widen K and V
+//   warps 12-15      split an item's Q, widen V
 // The work is cut into equal stretches of tiles, one per SM (rf_cache_attn.cuh); cut items are joined by a second kernel.
 #include <algorithm>
 
@@ -35,7 +44,7 @@ constexpr int kRows = 2 * BM, kThreads = 512;
 constexpr int kPagesWarp = 8, kMmaWarp = 9, kWidenWarp = 12;
 constexpr int kItemSlots = 2, kItemWords = 16, kItemReaders = 8;   // readers: the softmax warps
 constexpr int kRecords = 8, kBatch = 8;
-constexpr uint32_t kMore = 4, kLast = 8;
+constexpr uint32_t kMore = 4, kLast = 8, kFirst = 16;
 enum { kHeadPiece = 1, kTailPiece = 2 };
 // Register split: 2 x 128 softmax threads, 128 of the pages / MMA warpgroup, 128 that widen.  Checked like the clip kernel's
 // (see rf_regs_ok): against the register file here, against what the launch really owns on the host.
@@ -50,24 +59,23 @@ constexpr float kLazyRaise = 32.0f;                         // as in the clip ke
 constexpr float kRaise = 25.0f, kRaiseMargin = 8.0f;
 constexpr int kSpec = 32;
 
-// Shared memory, TMEM columns and operand layouts are those of the clip kernel (rf_attn.cu: Cfg), where they are explained: K and Q in
-// blocks of 64 columns with 128-byte swizzle, V in blocks of VBOX columns with a block of ones behind them whose product is
+// TMEM columns and V's layout are those of the clip kernel (rf_attn.cu: Cfg), where they are explained: V in blocks of VBOX columns with a block of ones behind them whose product is
 // the row sum of the rounded weights, P on top of S (D = 96 / 128) or in columns of its own (D = 64).
 template <int D>
 struct Cfg {
-  static constexpr int KB = (D + 63) / 64;
-  static constexpr uint32_t BLK = 128 * 128, TILE = KB * BLK;
+  // Q (its two parts) and K: 128 rows of PITCH bytes, swizzled by their pitch; at D = 96 the last 32 bytes are not used
+  static constexpr int PITCH = D == 64 ? 64 : 128;
+  static constexpr uint32_t TILE = 128 * PITCH;
+  static __host__ __device__ constexpr uint32_t qchunk(int row, int c) { return row * PITCH + ((D == 64 ? c ^ ((row >> 1) & 3) : c ^ (row & 7)) << 4); }
   static constexpr bool S_EARLY = D == 64;
-  static constexpr int NK = D == 64 ? 3 : 2, NV = NK;
-  static __host__ __device__ constexpr uint32_t koff(int ks) { return ks < 4 ? (uint32_t)ks * 32u : BLK + (uint32_t)(ks - 4) * 32u; }
+  static constexpr int NK = 3, NV = D == 64 ? 3 : 2;
   static constexpr int VBOX = D == 96 ? 32 : 64;
   static constexpr uint32_t VROW = VBOX * 2, VBLK = 128 * VROW, VLOAD = D / VBOX * VBLK, VTILE = VLOAD + VBLK;
   static constexpr int NPV = D + 16;
   static constexpr int PARTS = D == 64 ? 1 : 2;
   static __host__ __device__ constexpr int cut(int p) { return p * (BN / PARTS); }
   static __host__ __device__ constexpr uint32_t vchunk(int row, int c) { return row * VROW + ((VBOX == 64 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4); }
-  static __host__ __device__ constexpr uint32_t kchunk(int row, int c) { return (c >> 3) * BLK + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
-  static constexpr uint32_t Q = 0, K0 = 2 * TILE, V0 = K0 + NK * TILE, BAR = V0 + NV * VTILE;
+  static constexpr uint32_t Q = 0 /* stream 0 hi, lo, stream 1 hi, lo */, K0 = 4 * TILE, V0 = K0 + NK * TILE, BAR = V0 + NV * VTILE;
   static constexpr int B_Q = 0, B_QE = 1, B_KF = 2, B_KE = B_KF + NK, B_VF = B_KE + NK, B_VE = B_VF + NV, B_SF = B_VE + NV, B_PF = B_SF + 2,
                        B_OF = B_PF + 2 * PARTS, B_SE = B_OF + 2, B_IF = B_SE + 2, B_IE = B_IF + kItemSlots, B_RF = B_IE + kItemSlots,
                        B_RE = B_RF + kRecords, B_COUNT = B_RE + kRecords;
@@ -76,7 +84,8 @@ struct Cfg {
   static constexpr uint32_t RECORD = ITEM + kItemSlots * kItemWords * 4;    // kRecords of 8 words
   static constexpr uint32_t FLAGS = RECORD + kRecords * 32;                 // a tile's flags for the MMA thread, by K slot
   static constexpr uint32_t WINDOW = FLAGS + 16;                            // kBatch entries of the two lists, then a batch of the union
-  static constexpr uint32_t SCRATCH = WINDOW + 4 * kBatch * 4;
+  static constexpr uint32_t ROWSCALE = WINDOW + 4 * kBatch * 4;             // by item slot: what a row's parts were multiplied by, inverted
+  static constexpr uint32_t SCRATCH = ROWSCALE + kItemSlots * kRows * 4;
   static constexpr uint32_t TOTAL = SCRATCH + sizeof(StretchScratch);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
@@ -139,12 +148,12 @@ __device__ __forceinline__ void widen_place(int p, int warp, int lane, int& row,
   }
 }
 
-struct Maps { CUtensorMap q; };
+struct Maps { CUtensorMap k; };
 
 template <int D, bool LSE>
 __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
   using C = Cfg<D>;
-  constexpr uint32_t IDESC_S = idesc_bf16(BM, BN, 0), IDESC_PV = idesc_bf16(BM, C::NPV, 1);
+  constexpr uint32_t IDESC_HI = idesc_f8(BM, BN, 0), IDESC_LO = idesc_f8(BM, BN, 1), IDESC_PV = idesc_bf16(BM, C::NPV, 1);
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -157,12 +166,10 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    mbar_init(bar(C::B_Q), 1);
+    mbar_init(bar(C::B_Q), 4);
     mbar_init(bar(C::B_QE), 1);
-    for (int s = 0; s < C::NK; ++s) {
-      mbar_init(bar(C::B_KF + s), 4); mbar_init(bar(C::B_KE + s), 1);
-      mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1);
-    }
+    for (int s = 0; s < C::NK; ++s) { mbar_init(bar(C::B_KF + s), 1); mbar_init(bar(C::B_KE + s), 1); }
+    for (int s = 0; s < C::NV; ++s) { mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1); }
     for (int j = 0; j < 2; ++j) {
       mbar_init(bar(C::B_SF + j), 1);
       for (int p = 0; p < C::PARTS; ++p) mbar_init(bar(C::B_PF + j * C::PARTS + p), 4);
@@ -180,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   }
   fence_proxy_async_smem();
   if (warp == kPagesWarp) {
-    if (lane == 0) prefetch_tmap(&maps.q);
+    if (lane == 0) prefetch_tmap(&maps.k);
     __syncwarp();
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
   }
@@ -199,12 +206,63 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
 
   if (warp >= kWidenWarp) {
     RF_REGS_WIDEN();
-    // ------------------------------------------------------------ codes to bf16
+    // ------------------------------------------------------------ Q in two parts, V's codes to bf16
     constexpr int kPasses = D / 16;
-    const int w = warp - kWidenWarp;
+    const int w = warp - kWidenWarp, t = tid & 127;
     uint4 x[kPasses];
-    auto load = [&](const uint8_t* codes, uint32_t row_of_pages) {
-      const uint8_t* src = codes + (size_t)row_of_pages * (kPage * D);
+    // This thread's row of a stream's Q.  Rows that are not there become zeros.
+    auto split_q = [&](const int* iw, int slot, int j) {
+      const int r = iw[1] + j * BM + t;
+      const bool there = r < a.u.rows && r % a.u.M < iw[3];
+      const uint4* src = reinterpret_cast<const uint4*>(a.u.q + ((size_t)iw[0] * a.u.rows + (there ? r : 0)) * D);
+      uint32_t most = 0u;                     // largest magnitude, as bf16 bits
+#pragma unroll
+      for (int h = 0; h < D / 8; h += kPasses) {
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) x[p] = there ? src[h + p] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          const uint32_t* u = &x[p].x;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = max(most, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+        }
+      }
+      // times 2^e the largest lies in (224, 448]; a row with a value that is not finite gets that in its scale, so that its scores have it
+      int e = 8 - ((int)(most >> 7) - 127) - ((most & 127u) > 96u ? 1 : 0);
+      e = min(max(e, -126), 126);
+      const float up = most == 0u ? 1.f : __uint_as_float((uint32_t)(e + 127) << 23);
+      reinterpret_cast<float*>(base_ptr + C::ROWSCALE)[slot * kRows + j * BM + t] =
+          most >= 0x7f80u ? __uint_as_float(0x7fc00000u) : most == 0u ? 1.f : __uint_as_float((uint32_t)(127 - e) << 23);
+      const uint32_t hi_at = base + C::Q + j * 2 * C::TILE, lo_at = hi_at + C::TILE;
+#pragma unroll 1
+      for (int c = 0; c < D / 16; ++c) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const uint4 v = there ? src[2 * c + g] : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t* u = &v.x;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t hw = 0u, lw = 0u;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float f0 = __uint_as_float(u[2 * i + k] << 16) * up, f1 = __uint_as_float(u[2 * i + k] & 0xffff0000u) * up;
+              const uint32_t h2 = __nv_cvt_float2_to_fp8x2(make_float2(f0, f1), __NV_SATFINITE, __NV_E4M3);
+              const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3)));
+              const uint32_t l2 = __nv_cvt_float2_to_fp8x2(make_float2(f0 - back.x, f1 - back.y), __NV_SATFINITE, __NV_E5M2);
+              hw |= h2 << (16 * k);
+              lw |= l2 << (16 * k);
+            }
+            hi[2 * g + i] = hw;
+            lo[2 * g + i] = lw;
+          }
+        }
+        sts128(hi_at + C::qchunk(t, c), hi[0], hi[1], hi[2], hi[3]);
+        sts128(lo_at + C::qchunk(t, c), lo[0], lo[1], lo[2], lo[3]);
+      }
+    };
+    auto load = [&](uint32_t row_of_pages) {
+      const uint8_t* src = a.c.v + (size_t)row_of_pages * (kPage * D);
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         int row, c;
@@ -212,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         x[p] = *reinterpret_cast<const uint4*>(src + row * D + c * 16);
       }
     };
-    auto store = [&](bool keys, uint32_t to, uint32_t m1, uint32_t m2) {
+    auto store = [&](uint32_t to, uint32_t m1, uint32_t m2) {
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         int row, c;
@@ -221,52 +279,50 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         const uint32_t* in = &x[p].x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t t = __byte_perm(in[i], 0u, 0x3120);       // bytes 0 1 | 2 3 to where widen_even and widen_odd look
-          y[2 * i] = mul_bf16x2(widen_even(t), m1);
-          y[2 * i + 1] = mul_bf16x2(widen_odd(t), m1);
+          const uint32_t v = __byte_perm(in[i], 0u, 0x3120);       // bytes 0 1 | 2 3 to where widen_even and widen_odd look
+          y[2 * i] = mul_bf16x2(widen_even(v), m1);
+          y[2 * i + 1] = mul_bf16x2(widen_odd(v), m1);
         }
         if (m2 != kOne2) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = mul_bf16x2(y[i], m2);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t at;
-          if (keys) at = to + C::kchunk(row, 2 * c + i);
-          else at = to + (2 * c / (C::VBOX / 8)) * C::VBLK + C::vchunk(row, (2 * c + i) % (C::VBOX / 8));
-          sts128(at, y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-        }
+        for (int i = 0; i < 2; ++i)
+          sts128(to + (2 * c / (C::VBOX / 8)) * C::VBLK + C::vchunk(row, (2 * c + i) % (C::VBOX / 8)), y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
       }
       fence_proxy_async_smem();
       __syncwarp();
     };
-    bool ok = true;
+    int nq = 0;
     for (int u = 0;; ++u) {
-      const int slot = u % kRecords, ks = u % C::NK;
-      ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RF + slot), (u / kRecords) & 1, wc, 0));
-      if (!ok) break;
+      const int slot = u % kRecords, vs = u % C::NV;
+      if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RF + slot), (u / kRecords) & 1, wc, 0))) break;
       volatile const uint32_t* r = records + slot * 8;
-      const uint32_t f = r[0], row = r[1], k1 = r[2], k2 = r[3], v1 = r[4], v2 = r[5];
-      if (f & kMore) load(a.c.k, row);
-      if (u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc));
-      if (!ok) break;
-      if (f & kMore) store(true, base + C::K0 + ks * C::TILE, k1, k2);
-      if (w == 0 && lane == 0) flags[ks] = f;
-      if (lane == 0) mbar_arrive(bar(C::B_KF + ks));
+      const uint32_t f = r[0], row = r[1], v1 = r[2], v2 = r[3];
       if (!(f & kMore)) break;
-      load(a.c.v, row);
+      if (f & kFirst) {
+        const int is = (int)r[4];
+        if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(C::B_QE), (nq - 1) & 1, wc))) break;   // the item before has taken its last scores
+        ++nq;
+        split_q(items + is * kItemWords, is, 0);
+        split_q(items + is * kItemWords, is, 1);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::B_Q));
+      }
+      load(row);
       if (lane == 0) mbar_arrive(bar(C::B_RE + slot));
-      if (u >= C::NV) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_VE + ks), ((u / C::NV) - 1) & 1, wc));
-      if (!ok) break;
-      store(false, base + C::V0 + ks * C::VTILE, v1, v2);
-      if (lane == 0) mbar_arrive(bar(C::B_VF + ks));
+      if (u >= C::NV && !__all_sync(0xffffffffu, mbar_wait(bar(C::B_VE + vs), ((u / C::NV) - 1) & 1, wc))) break;
+      store(base + C::V0 + vs * C::VTILE, v1, v2);
+      if (lane == 0) mbar_arrive(bar(C::B_VF + vs));
     }
   } else if (warp >= kPagesWarp) {
     RF_REGS_CONTROL();
     if (warp == kPagesWarp) {
       // ------------------------------------------------------------ pages
       int* win = reinterpret_cast<int*>(base_ptr + C::WINDOW);
-      int no = 0, u = 0, nq = 0;          // items published, tiles published, Q fetched
+      int no = 0, u = 0;                  // items published, tiles published
       long long at = st.at;
       int item = st.item;
       bool ok = true;
@@ -296,17 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         at += n;
         pos = at;
         if (e0 == b0 && e1 == b1) continue;                    // sees nothing, or lists nothing here
-        if (nq > 0) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QE), (nq - 1) & 1, wc, end - begin));
-        if (!ok) break;
-        if (lane == 0) {
-          mbar_expect_tx(bar(C::B_Q), 2 * C::TILE);
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int kb = 0; kb < C::KB; ++kb)
-              tma_load_3d(base + C::Q + j * C::TILE + kb * C::BLK, &maps.q, kb * 64, it.r0 + j * BM, it.bh, bar(C::B_Q));
-        }
-        ++nq;
+        bool first = true;
         const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
         const int32_t* l1 = l0 != nullptr && it.r0 / kPage + 1 < a.u.n_q ? l0 + a.n_k : l0;
         int i0 = b0, i1 = b1;
@@ -341,59 +387,70 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           i0 += take0;
           i1 += take1;
           uint32_t row = 0, f = 0;
-          rf_cache_attn::Widen kw = {kOne2, kOne2}, vw = kw;
+          rf_cache_attn::Widen vw = {kOne2, kOne2};
           if (lane < cnt) {
             const int page = win[2 * kBatch + lane];
             f = (uint32_t)win[3 * kBatch + lane] | kMore;
             if (lane == cnt - 1 && i0 == e0 && i1 == e1) f |= kLast;
+            if (lane == 0 && first) f |= kFirst;
             const int phys = rf_page(a.c, it.b, min(page, pages - 1), a.dev_status);   // (a page that no row sees: any will do)
             row = (uint32_t)phys * a.c.H + it.bh % a.c.H;
-            prefetch_l2(a.c.k + (size_t)row * (kPage * D), kPage * D);
             prefetch_l2(a.c.v + (size_t)row * (kPage * D), kPage * D);
-            kw = rf_cache_attn::widen_by(a.c.k_scale[row]);
             vw = rf_cache_attn::widen_by(a.c.v_scale[row]);
           }
-          // the records' slots one after the other, each filled by the lane that looked it up
+          first = false;
+          // the tiles one after the other, each by the lane that looked it up: V's record, then K
           for (int i = 0; i < cnt && ok; ++i, ++u) {
-            const int rs = u % kRecords;
+            const int rs = u % kRecords, ks = u % C::NK;
             if (u >= kRecords) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0));
             if (ok && lane == i) {
               volatile uint32_t* r = records + rs * 8;
-              r[0] = f; r[1] = row; r[2] = kw.m1; r[3] = kw.m2; r[4] = vw.m1; r[5] = vw.m2;
+              r[0] = f; r[1] = row; r[2] = vw.m1; r[3] = vw.m2; r[4] = slot;
               mbar_arrive(bar(C::B_RF + rs));
+            }
+            if (ok && u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0));
+            if (ok && lane == i) {
+              flags[ks] = f;
+              mbar_expect_tx(bar(C::B_KF + ks), C::TILE);
+              tma_load_3d(base + C::K0 + ks * C::TILE, &maps.k, 0, 0, (int)row, bar(C::B_KF + ks));
             }
           }
           __syncwarp();
         }
       }
       // the end, for the warps that walk tiles and for those that walk items
-      const int rs = u % kRecords, slot = no % kItemSlots;
+      const int rs = u % kRecords, slot = no % kItemSlots, ks = u % C::NK;
+      if (u >= C::NK) mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0);
       if (u >= kRecords) mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0);
       if (no >= kItemSlots) mbar_wait_long(bar(C::B_IE + slot), ((no / kItemSlots) - 1) & 1, wc, (int)min(st.hi - st.lo, 1ll << 20));
       if (lane == 0) {
         records[rs * 8] = 0;
         mbar_arrive(bar(C::B_RF + rs));
+        flags[ks] = 0;
+        mbar_arrive(bar(C::B_KF + ks));
         items[slot * kItemWords] = -1;
         mbar_arrive(bar(C::B_IF + slot));
       }
     } else if (warp == kMmaWarp) {
       // ------------------------------------------------------------ MMA issuer
       if (C::S_EARLY ? lane == 0 : elect_one()) {
-        constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
-        constexpr uint32_t DESC_HI_V = C::VBOX == 64 ? DESC_HI : (512u >> 4) | (1u << 14) | (4u << 29);
+        constexpr uint32_t SW128 = (1024u >> 4) | (1u << 14) | (2u << 29), SW64 = (512u >> 4) | (1u << 14) | (4u << 29);   // stride of 8 rows, version, swizzle
+        constexpr uint32_t DESC_HI = C::PITCH == 128 ? SW128 : SW64, DESC_HI_V = C::VBOX == 64 ? SW128 : SW64;
         constexpr uint32_t LO_KMAJOR = 1u << 16, LO_VMAJOR = (C::VBLK >> 4) << 16;
         auto desc = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI << 32) | lo; };
         auto desc_v = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI_V << 32) | lo; };
         const uint32_t q_lo = ((base + C::Q) >> 4) | LO_KMAJOR, k_lo = ((base + C::K0) >> 4) | LO_KMAJOR;
         const uint32_t v_lo = ((base + C::V0) >> 4) | LO_VMAJOR;
         auto issue_s = [&](int j, int ks) {
-          uint32_t a0 = q_lo + j * (C::TILE >> 4);
+          uint32_t a0 = q_lo + 2 * j * (C::TILE >> 4);
           const uint32_t b0 = k_lo + ks * (C::TILE >> 4);
           asm volatile("" : "+r"(a0));
           const uint32_t t_d = tmem_base + (j ? C::S_COL1 : C::S_COL0);
-          mma_ss_c<false>(t_d, desc(a0), desc(b0), IDESC_S);
+          mma_f8_c<false>(t_d, desc(a0), desc(b0), IDESC_HI);
 #pragma unroll
-          for (int k = 1; k < D / 16; ++k) mma_ss_c<true>(t_d, desc(a0 + (C::koff(k) >> 4)), desc(b0 + (C::koff(k) >> 4)), IDESC_S);
+          for (int k = 1; k < D / 32; ++k) mma_f8_c<true>(t_d, desc(a0 + k * 2), desc(b0 + k * 2), IDESC_HI);
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) mma_f8_c<true>(t_d, desc(a0 + (C::TILE >> 4) + k * 2), desc(b0 + k * 2), IDESC_LO);
           tc_commit(bar(C::B_SF + j));
         };
         auto issue_pv = [&](int j, int vs, uint32_t acc, uint32_t par) {
@@ -496,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     const uint32_t t_s = tmem_base + lane_sel + (j ? C::S_COL1 : C::S_COL0);
     const uint32_t t_o = tmem_base + lane_sel + (j ? C::O_COL1 : C::O_COL0);
     const float sc = a.scale_log2;
-    uint32_t done = 0;
+    uint32_t done = 0, nq = 0;
     int waited = 0;
     for (int item = 0;; ++item) {
       const int slot = item % kItemSlots;
@@ -510,11 +567,36 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       if (r < a.u.rows && r % a.u.M < iw[3]) sees = rf_row_sees(a.u.causal, iw[2], iw[3], r % a.u.M);
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)iw[0] * a.u.n_q + min(iw[1] / kPage + j, a.u.n_q - 1)) * a.n_k : nullptr;
       float m_run = -INFINITY, l_run = 0.f, l_exact = 0.f;
+      // The factor of a tile's scores holds the page's scale: the page is looked up two tiles ahead, its scale one.
+      const int32_t* table = a.c.table + (size_t)(iw[0] / a.c.H) * a.c.max_pages;
+      const float* k_scale = a.c.k_scale + iw[0] % a.c.H;
+      auto page_of = [&](int t) -> int {
+        const int p = list != nullptr ? list[t] : t;
+        return p < 0 || p >= pages ? pages : p;
+      };
+      auto place_of = [&](int page) -> int { return min(max(table[min(page, pages - 1)], 0), a.c.n_pages - 1); };
+      float row_scale = sc, ks_next = 0.f;
+      int page_next = 0, place_next = 0;
+      if (n > 0) {
+        page_next = page_of(begin);
+        ks_next = k_scale[(size_t)place_of(page_next) * a.c.H];
+        if (n > 1) place_next = place_of(page_of(begin + 1));
+      }
+      if (waited > 0) {
+        mbar_wait(bar(C::B_Q), nq & 1, wc);
+        ++nq;
+        row_scale *= reinterpret_cast<const float*>(base_ptr + C::ROWSCALE)[slot * kRows + j * BM + row_in_tile];
+      }
       bool opens = true;
       for (int t = begin; t < end; ++t, ++done, opens = false) {
-        int page = list != nullptr ? list[t] : t;
-        if (page < 0 || page >= pages) page = pages;
-        const int left = sees - page * kPage;             // keys of the tile that this row sees (page <= 2^23: no overflow)
+        const int left = sees - page_next * kPage;        // keys of the tile that this row sees (page <= 2^23: no overflow)
+        float sc = row_scale * ks_next;
+        if (sc < 1.1754944e-38f) sc = 1.1754944e-38f;     // (a masked score, -inf, times zero would be no number)
+        if (t + 1 < end) {
+          page_next = page_of(t + 1);
+          ks_next = k_scale[(size_t)place_next * a.c.H];
+          if (t + 2 < end) place_next = place_of(page_of(t + 2));
+        }
         const bool partial = __any_sync(0xffffffffu, left < BN);
         mbar_wait(bar(C::B_SF + j), done & 1, wc);
         tc_fence_after();
@@ -766,7 +848,7 @@ rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
     configured[dev] = true;
   }
   Maps maps;
-  if (!rf_encode_rows_map(&maps.q, a.u.q, D, a.u.rows, (size_t)D * 2, (size_t)a.u.rows * D * 2, a.c.B * a.c.H)) return RF_ERR_CUDA;
+  if (!rf_encode_pages_map(&maps.k, a.c.k, a.c)) return RF_ERR_CUDA;
   const int ctas = chunk_ctas(a.c, a.u);
   if (rf_launch(rf_cache_chunk_kernel<D, LSE>, dim3(ctas), kThreads, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
   if (ctas == 1) return RF_OK;

@@ -203,6 +203,20 @@ __device__ __forceinline__ void mma_ts_c(uint32_t d_tmem, uint32_t a_tmem, uint6
       : "memory");
 }
 
+// Instruction descriptor, kind::f8f6f4: A e4m3 (0) or e5m2 (1), B e4m3, both K-major, -> fp32.  32 columns an instruction.
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, int a_e5m2) {
+  return (1u << 4) | ((uint32_t)a_e5m2 << 7) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+template <bool ACC>
+__device__ __forceinline__ void mma_f8_c(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.eq.u32 p, %4, 1;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "n"(ACC ? 1 : 0)
+      : "memory");
+}
+
 // 32 consecutive fp32 columns of this thread's TMEM lane (lane = 32*(warp%4) + laneid).
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&v)[32]) {
   asm volatile(

@@ -88,10 +88,11 @@ class Pair:
         return o, l
 
 
-def check_attention(o, lse, ref, ref_lse, spread, reach, model, q_len, what=""):
+def check_attention(o, lse, ref, ref_lse, spread, reach, wide, model, q_len, what=""):
     """o (bf16) and lse (fp32) against fp64.  With s a score in nats, its error is at most the fp32 sums' of D exact products of
     bf16 numbers, the scaling's and the maximum's subtraction: (D + 8) * 2^-24 * sum |q k| scale =: e_s, and an exponential adds
-    2^-21.  Each weight is rounded to bf16 (2^-8 of itself) and O is the mean of V under the rounded weights, so the error of
+    2^-21; chunks take a query row as two 8-bit numbers that miss an element by 2^-21.8 of the row's largest at most, which adds 2^-21 *
+    max |q| * scale * sum |k| (`wide`).  Each weight is rounded to bf16 (2^-8 of itself) and O is the mean of V under the rounded weights, so the error of
     an element is at most (2^-8 + e_s + 2^-21) * (sum w |v| + |o|), times 1 / (1 - 2^-8), plus the fp32 sums of n terms, n * 2^-24 of sum
     w |v|, plus the rounding of o itself.  The log-sum-exp has e_s, the exponentials and the fp32 sum of n positive terms, and
     its own rounding."""
@@ -100,7 +101,7 @@ def check_attention(o, lse, ref, ref_lse, spread, reach, model, q_len, what=""):
     for b in range(B):
         n = model.len[b]
         at = (b, slice(None), slice(0, q_len[b]))
-        e_s = ((D + 8) * FP32 * reach[at] + 2.0 ** -21)
+        e_s = ((D + 8) * FP32 * reach[at] + 2.0 ** -21 * wide[at] + 2.0 ** -21)
         mass = spread[at] + np.abs(ref[at])
         bound = (BF16 + e_s[..., None]) * mass * (1 + 2 * BF16) + n * FP32 * spread[at] + BF16 * np.abs(ref[at]) + 1e-37
         err = np.abs(got[at] - ref[at])

@@ -48,7 +48,7 @@ def test_attention_equals_torch_on_the_stored_tokens():
     c.append(k, v, [150, 40])
     q = rng.standard_normal((2, 4, 10, 8))
     for causal in (0, 1, 7):
-        o, lse, _, _ = c.attend(q, [10, 10], causal)
+        o, lse, *_ = c.attend(q, [10, 10], causal)
         for b in range(2):
             L = c.len[b]
             p = torch.arange(10) + L - 10
@@ -68,7 +68,7 @@ def test_selecting_every_page_is_attending_to_all_and_rows_can_be_empty():
     lists = c.select(q, [140], 0, 0, 0, 3)
     assert lists == [[[[0, 1, 2], [0, 1, 2]]]]
     assert np.array_equal(c.attend(q, [140])[0], c.attend(q, [140], lists=lists)[0])
-    o, lse, _, _ = c.attend(q, [140], lists=[[[[], [1]]]])
+    o, lse, *_ = c.attend(q, [140], lists=[[[[], [1]]]])
     assert np.all(o[0, 0, :128] == 0) and np.all(np.isneginf(lse[0, 0, :128])) and np.all(np.isfinite(lse[0, 0, 128:]))
     # identical pages: the lower one
     c.append(np.zeros((1, 1, 84, 8)), np.zeros((1, 1, 84, 8)), [84])
