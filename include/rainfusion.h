@@ -417,7 +417,7 @@ rf_status rf_cache_compact(const rf_cache *cache, int32_t *n_live, void *ws, siz
 /*
  * Queries of a call on the cache.  q is bf16 [n_seqs, H, M, D]; H is a multiple of cache->heads, and heads g * H / heads .. of q
  * share K/V head g.  Sequence b has q_len[b] <= M query rows: the last q_len[b] tokens of the sequence (which are in the cache already),
- * row i at position p = seq_len[b] - q_len[b] + i.  Rows from q_len[b] on are padding: not read, and their outputs are not written.
+ * row i at position p = seq_len[b] - q_len[b] + i.  Rows from q_len[b] on are padding: what they hold does not matter, and their outputs are not written.
  * With causal_block = c > 0 a row sees the keys of its own block of c positions and of the blocks before: positions below
  * (p / c + 1) * c (c = tokens of a frame: frame by frame; 1: token by token), none if p < 0.  c = 0: every key.
  * The rows of a K/V head, [H / heads * M] one query head after the other, are cut into tiles of RF_CACHE_PAGE rows; a

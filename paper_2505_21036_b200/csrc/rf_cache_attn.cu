@@ -60,8 +60,11 @@ __device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem&
   return a.count == nullptr ? rf_pages(it.sees) : listed(a, it, it.r0 / kPage);
 }
 struct TokenPlaces {
-  static constexpr int kRowsOf = kRows;
-  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) { return places(item_tiles(a, cache_item<kRows>(a, item))); }
+  static constexpr int kRowsOf = kRows, kEnd = 2;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
+  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+    const int n = item_tiles(a, cache_item<kRows>(a, item));
+    return n < 0 ? 0 : n + kEnd;
+  }
 };
 
 struct Maps { CUtensorMap k, v; };
@@ -94,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
   if (tid == 0) {
     int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
     head[0] = st.item;
-    head[3] = st.lo < st.hi && st.at < st.lo;
+    head[3] = st.cuts;
   }
 
   if (warp == kWarps) {
@@ -121,9 +124,12 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
     };
     for (long long pos = st.lo; pos < st.hi; ++item) {
       const CacheItem it = cache_item<kRows>(a, item);
-      const int tiles = item_tiles(a, it), n = places(tiles);
-      if (n == 0) continue;
-      const int begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+      const int tiles = item_tiles(a, it);
+      if (tiles < 0) continue;
+      const int n = max(tiles, 1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+      at += tiles + TokenPlaces::kEnd;
+      pos = min(at, st.hi);
+      if (begin >= n) continue;                          // only the places of the item's end
       const int cut = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
       const int pages = rf_pages(it.len);
@@ -165,8 +171,6 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
           step();
         }
       }
-      at += n;
-      pos = at;
     }
     if (lane == 0) publish(Record{0, 0, kEnd, 0, 0, 0, 0, 0}, false, 0);
   } else {

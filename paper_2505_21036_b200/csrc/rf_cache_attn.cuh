@@ -35,14 +35,14 @@ __device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) 
 __device__ __forceinline__ int listed(const RfCacheAttn& a, const CacheItem& it, int tile) {
   return it.len == 0 ? 0 : min(max(a.count[(size_t)it.bh * a.u.n_q + tile], 0), a.n_k);
 }
-// A row block that sees nothing has a place on the line too: its outputs are written.
-__device__ __forceinline__ int places(int tiles) { return tiles < 0 ? 0 : max(tiles, 1); }
-
-// A CTA's stretch [lo, hi) of the line, and the item that lo lies in (which begins at place `at`).
-struct Stretch { long long lo, hi, at; int item; };
+// A CTA's stretch [lo, hi) of the line, and the item that lo lies in (which begins at place `at`; behind the places of its tiles lie
+// some that stand for what an item costs beside them, at least one, so that a row block that sees nothing has its outputs written).
+// cuts: lo lies among that item's tiles, behind the first.
+struct Stretch { long long lo, hi, at; int item, cuts; };
 struct StretchScratch { long long sums[33]; Stretch st; };
 
-// Called by all threads of the CTA (kThreads of them, whole warps).  Places::of(a, item): the item's places on the line.
+// Called by all threads of the CTA (kThreads of them, whole warps).  Places::of(a, item): the item's places on the line, kEnd of
+// them at its end for itself; 0 for an item whose rows are all padding.
 template <typename Places, int kThreads>
 __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch* s) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -66,16 +66,18 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
   // no more stretches than places: the ones in use are the first, and none of them is empty
   const long long n = min((long long)gridDim.x, max(total, 1ll)), x0 = min((long long)blockIdx.x, n), x1 = min(x0 + 1, n);
   const long long lo = total * x0 / n, hi = total * x1 / n;
-  if (tid == 0 && lo == hi) s->st = Stretch{lo, hi, lo, items};
+  if (tid == 0 && lo == hi) s->st = Stretch{lo, hi, lo, items, 0};
   if (lo < hi && before <= lo && lo < before + mine) {
     long long at = before;
     int i = i0;
     for (;; ++i) {
       const int p = Places::of(a, i);
-      if (lo < at + p) break;
+      if (lo < at + p) {
+        s->st = Stretch{lo, hi, at, i, at < lo && lo < at + p - Places::kEnd};
+        break;
+      }
       at += p;
     }
-    s->st = Stretch{lo, hi, at, i};
   }
   __syncthreads();
   return s->st;

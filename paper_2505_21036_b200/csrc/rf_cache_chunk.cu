@@ -16,9 +16,12 @@
 // 1090 us.)
 // Warp roles:
 //   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
-//   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches K by TMA
+//   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q and the codes by TMA
 //   warp 9           issues the tcgen05.mma
 //   warps 12-15      split an item's Q, widen V
+// The last group's code is kept short, in rolled loops over shared memory: beside the softmax's two thousand instructions long stretches
+// of straight code come in from the L2 line by line.  (Q split in unrolled code from global loads: 25 000 cycles an item, most of them
+// waits for instructions.)
 // The work is cut into equal stretches of tiles, one per SM (rf_cache_attn.cuh); cut items are joined by a second kernel.
 #include <algorithm>
 
@@ -36,14 +39,13 @@ using rf_cache_attn::head_floats;
 using rf_cache_attn::kHeadWords;
 using rf_cache_attn::kOne2;
 using rf_cache_attn::mul_bf16x2;
-using rf_cache_attn::places;
 using rf_cache_attn::widen_even;
 using rf_cache_attn::widen_odd;
 
 constexpr int kRows = 2 * BM, kThreads = 512;
 constexpr int kPagesWarp = 8, kMmaWarp = 9, kWidenWarp = 12;
 constexpr int kItemSlots = 2, kItemWords = 16, kItemReaders = 8;   // readers: the softmax warps
-constexpr int kRecords = 8, kBatch = 8;
+constexpr int kBatch = 8, kUnroll = 2;
 constexpr uint32_t kMore = 4, kLast = 8, kFirst = 16;
 enum { kHeadPiece = 1, kTailPiece = 2 };
 // Register split: 2 x 128 softmax threads, 128 of the pages / MMA warpgroup, 128 that widen.  Checked like the clip kernel's
@@ -68,24 +70,27 @@ struct Cfg {
   static constexpr uint32_t TILE = 128 * PITCH;
   static __host__ __device__ constexpr uint32_t qchunk(int row, int c) { return row * PITCH + ((D == 64 ? c ^ ((row >> 1) & 3) : c ^ (row & 7)) << 4); }
   static constexpr bool S_EARLY = D == 64;
-  static constexpr int NK = 3, NV = D == 64 ? 3 : 2;
+  static constexpr int NK = D == 128 ? 2 : 3, NV = D == 64 ? 3 : 2, NS = 2;    // slots of K, of V, of V's codes
   static constexpr int VBOX = D == 96 ? 32 : 64;
   static constexpr uint32_t VROW = VBOX * 2, VBLK = 128 * VROW, VLOAD = D / VBOX * VBLK, VTILE = VLOAD + VBLK;
   static constexpr int NPV = D + 16;
   static constexpr int PARTS = D == 64 ? 1 : 2;
   static __host__ __device__ constexpr int cut(int p) { return p * (BN / PARTS); }
   static __host__ __device__ constexpr uint32_t vchunk(int row, int c) { return row * VROW + ((VBOX == 64 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4); }
-  static constexpr uint32_t Q = 0 /* stream 0 hi, lo, stream 1 hi, lo */, K0 = 4 * TILE, V0 = K0 + NK * TILE, BAR = V0 + NV * VTILE;
-  static constexpr int B_Q = 0, B_QE = 1, B_KF = 2, B_KE = B_KF + NK, B_VF = B_KE + NK, B_VE = B_VF + NV, B_SF = B_VE + NV, B_PF = B_SF + 2,
-                       B_OF = B_PF + 2 * PARTS, B_SE = B_OF + 2, B_IF = B_SE + 2, B_IE = B_IF + kItemSlots, B_RF = B_IE + kItemSlots,
-                       B_RE = B_RF + kRecords, B_COUNT = B_RE + kRecords;
+  // Q: stream 0 hi, lo, stream 1 hi, lo; the rows come in as bf16 in the same place, 64 columns where hi goes and the others where lo goes,
+  // or at D = 64 in a place of their own
+  static constexpr uint32_t Q = 0, RAW = 4 * TILE, K0 = RAW + (D == 64 ? 2 * 128 * 128 : 0), VS0 = K0 + NK * TILE, V0 = VS0 + NS * TILE, BAR = V0 + NV * VTILE;
+  static constexpr int B_Q = 0, B_QE = 1, B_QR = 2, B_KF = 3, B_KE = B_KF + NK, B_VF = B_KE + NK, B_VE = B_VF + NV, B_SF = B_VE + NV, B_PF = B_SF + 2,
+                       B_OF = B_PF + 2 * PARTS, B_SE = B_OF + 2, B_IF = B_SE + 2, B_IE = B_IF + kItemSlots, B_CF = B_IE + kItemSlots,
+                       B_CE = B_CF + NS, B_COUNT = B_CE + NS;
   static constexpr uint32_t MISC = BAR + 8 * B_COUNT;
   static constexpr uint32_t ITEM = (MISC + 16 + 15) / 16 * 16;
-  static constexpr uint32_t RECORD = ITEM + kItemSlots * kItemWords * 4;    // kRecords of 8 words
-  static constexpr uint32_t FLAGS = RECORD + kRecords * 32;                 // a tile's flags for the MMA thread, by K slot
+  static constexpr uint32_t RECORD = ITEM + kItemSlots * kItemWords * 4;    // what goes with a slot of V's codes: 4 words
+  static constexpr uint32_t FLAGS = RECORD + NS * 16;                       // a tile's flags for the MMA thread, by K slot
   static constexpr uint32_t WINDOW = FLAGS + 16;                            // kBatch entries of the two lists, then a batch of the union
-  static constexpr uint32_t ROWSCALE = WINDOW + 4 * kBatch * 4;             // by item slot: what a row's parts were multiplied by, inverted
-  static constexpr uint32_t SCRATCH = ROWSCALE + kItemSlots * kRows * 4;
+  static constexpr uint32_t ROWEXP = WINDOW + 4 * kBatch * 4;               // by item slot: exponent field of what undoes a row's scaling
+  static_assert(ROWEXP % 8 == 0 && (ROWEXP + kItemSlots * kRows) % 8 == 0, "alignment");
+  static constexpr uint32_t SCRATCH = ROWEXP + kItemSlots * kRows;
   static constexpr uint32_t TOTAL = SCRATCH + sizeof(StretchScratch);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
@@ -97,7 +102,10 @@ struct Cfg {
   static constexpr size_t PIECE = (size_t)(D / 4 + 1) * BM;                 // float4 of one piece of one stream: O, then {m, l, l exact, has O}
 };
 
-// The two streams' lists of an item: how long they are and how many places of the line the item takes.
+// What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
+constexpr int kItemPlaces = 4;
+
+// The two streams' lists of an item: how long they are, how many keys their rows see at most.
 struct Streams { int n0, n1, sees0, sees1; };
 __device__ __forceinline__ Streams streams(const RfCacheAttn& a, const CacheItem& it) {
   Streams s;
@@ -114,41 +122,44 @@ __device__ __forceinline__ Streams streams(const RfCacheAttn& a, const CacheItem
   return s;
 }
 struct ChunkPlaces {
-  static constexpr int kRowsOf = kRows;
+  static constexpr int kRowsOf = kRows, kEnd = kItemPlaces;
   static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
     const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
     if (it.sees < 0) return 0;
     const Streams s = streams(a, it);
-    return places(max(s.n0, s.n1));
+    return max(s.n0, s.n1) + kItemPlaces;
   }
 };
 
-struct Item { int bh, r0, len, q_len, pages, n0, n1, b0, b1, cut; };
-
-__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
+__device__ __forceinline__ void sts64(uint32_t at, uint32_t x, uint32_t y) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
+}
 
-// Which 16-byte chunk of codes a thread of the widening warps takes in pass p: eight neighbouring lanes write eight
-// different 16-byte columns of shared memory (nearly so at D = 96).
+// Which 16-byte chunk of codes a thread of the widening warps takes in pass p: eight neighbouring lanes read and write eight
+// different 16-byte columns of shared memory (rows r and r ^ 5 differ in both swizzles; nearly so at D = 96).
 template <int D>
 __device__ __forceinline__ void widen_place(int p, int warp, int lane, int& row, int& c) {
+  const int five = (lane >> 2) & 1 ? 5 : 0;
   if (D == 128) {
-    row = p * 16 + warp * 4 + ((lane >> 4) & 1) * 2 + ((lane >> 2) & 1);
+    row = (p >> 1) * 32 + warp * 8 + ((((lane >> 4) & 1) | ((p & 1) << 1)) ^ five);
     c = ((lane >> 3) & 1) * 4 + (lane & 3);
-  } else if (D == 64 || p < 4) {
+  } else if (D == 64) {
     row = p * 32 + warp * 8 + (lane >> 2);
     c = lane & 3;
+  } else if (p < 4) {
+    row = p * 32 + warp * 8 + (((lane >> 3) & 3) ^ five);
+    c = lane & 3;
   } else {
-    row = (p - 4) * 64 + warp * 16 + (lane >> 1);
+    const int i = lane >> 1;
+    row = (p - 4) * 64 + warp * 16 + (((i & 3) << 1) | ((i >> 2) & 1) | (i & 8));
     c = 4 + (lane & 1);
   }
 }
 
-struct Maps { CUtensorMap k; };
+struct Maps { CUtensorMap q, k, v; };
 
 template <int D, bool LSE>
 __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
@@ -168,6 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   if (tid == 0) {
     mbar_init(bar(C::B_Q), 4);
     mbar_init(bar(C::B_QE), 1);
+    mbar_init(bar(C::B_QR), 1);
     for (int s = 0; s < C::NK; ++s) { mbar_init(bar(C::B_KF + s), 1); mbar_init(bar(C::B_KE + s), 1); }
     for (int s = 0; s < C::NV; ++s) { mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1); }
     for (int j = 0; j < 2; ++j) {
@@ -177,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       mbar_init(bar(C::B_SE + j), 4);
     }
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(bar(C::B_IF + i), 1); mbar_init(bar(C::B_IE + i), kItemReaders); }
-    for (int i = 0; i < kRecords; ++i) { mbar_init(bar(C::B_RF + i), 1); mbar_init(bar(C::B_RE + i), 4); }
+    for (int i = 0; i < C::NS; ++i) { mbar_init(bar(C::B_CF + i), 1); mbar_init(bar(C::B_CE + i), 4); }
     *abort_flag = 0;
     mbar_init_fence();
   }
@@ -187,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   }
   fence_proxy_async_smem();
   if (warp == kPagesWarp) {
-    if (lane == 0) prefetch_tmap(&maps.k);
+    if (lane == 0) { prefetch_tmap(&maps.q); prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
     __syncwarp();
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
   }
@@ -201,87 +213,90 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   if (tid == 0) {
     int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
     head[0] = st.item;
-    head[3] = st.lo < st.hi && st.at < st.lo;
+    head[3] = st.cuts;
   }
 
   if (warp >= kWidenWarp) {
     RF_REGS_WIDEN();
     // ------------------------------------------------------------ Q in two parts, V's codes to bf16
-    constexpr int kPasses = D / 16;
-    const int w = warp - kWidenWarp, t = tid & 127;
-    uint4 x[kPasses];
-    // This thread's row of a stream's Q.  Rows that are not there become zeros.
-    auto split_q = [&](const int* iw, int slot, int j) {
-      const int r = iw[1] + j * BM + t;
-      const bool there = r < a.u.rows && r % a.u.M < iw[3];
-      const uint4* src = reinterpret_cast<const uint4*>(a.u.q + ((size_t)iw[0] * a.u.rows + (there ? r : 0)) * D);
-      uint32_t most = 0u;                     // largest magnitude, as bf16 bits
-#pragma unroll
-      for (int h = 0; h < D / 8; h += kPasses) {
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) x[p] = there ? src[h + p] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          const uint32_t* u = &x[p].x;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) most = max(most, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
-        }
-      }
-      // times 2^e the largest lies in (224, 448]; a row with a value that is not finite gets that in its scale, so that its scores have it
-      int e = 8 - ((int)(most >> 7) - 127) - ((most & 127u) > 96u ? 1 : 0);
-      e = min(max(e, -126), 126);
-      const float up = most == 0u ? 1.f : __uint_as_float((uint32_t)(e + 127) << 23);
-      reinterpret_cast<float*>(base_ptr + C::ROWSCALE)[slot * kRows + j * BM + t] =
-          most >= 0x7f80u ? __uint_as_float(0x7fc00000u) : most == 0u ? 1.f : __uint_as_float((uint32_t)(127 - e) << 23);
-      const uint32_t hi_at = base + C::Q + j * 2 * C::TILE, lo_at = hi_at + C::TILE;
+    const int w = warp - kWidenWarp;
+    // An item's 256 rows, kLanes neighbouring lanes a row (16 bytes each), in place: a warp has read its rows before it writes their parts.
+    auto split_q = [&](int slot) {
+      constexpr int kLanes = D == 64 ? 8 : 16, kRowsAtOnce = 32 / kLanes, kTogether = 2;
+      const int c = lane % kLanes;
 #pragma unroll 1
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t hi[4], lo[4];
+      for (int s0 = w * kRowsAtOnce + lane / kLanes; s0 < kRows; s0 += 4 * kRowsAtOnce * kTogether) {
+        uint4 v[kTogether];
+        uint32_t most[kTogether];             // the rows' largest magnitudes, as bf16 bits
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const uint4 v = there ? src[2 * c + g] : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t* u = &v.x;
+        for (int k = 0; k < kTogether; ++k) {
+          const int j = (s0 + k * 4 * kRowsAtOnce) >> 7, row = (s0 + k * 4 * kRowsAtOnce) & 127;
+          const uint32_t at = D == 64 ? C::RAW + j * 128 * 128 : C::Q + (2 * j + (c >> 3)) * C::TILE;
+          v[k] = c < D / 8 ? *reinterpret_cast<const uint4*>(base_ptr + at + row * 128 + (((c & 7) ^ (row & 7)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t* u = &v[k].x;
+          most[k] = 0u;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t hw = 0u, lw = 0u;
+          for (int i = 0; i < 4; ++i) most[k] = max(most[k], max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+        }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float f0 = __uint_as_float(u[2 * i + k] << 16) * up, f1 = __uint_as_float(u[2 * i + k] & 0xffff0000u) * up;
-              const uint32_t h2 = __nv_cvt_float2_to_fp8x2(make_float2(f0, f1), __NV_SATFINITE, __NV_E4M3);
-              const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3)));
-              const uint32_t l2 = __nv_cvt_float2_to_fp8x2(make_float2(f0 - back.x, f1 - back.y), __NV_SATFINITE, __NV_E5M2);
-              hw |= h2 << (16 * k);
-              lw |= l2 << (16 * k);
-            }
-            hi[2 * g + i] = hw;
-            lo[2 * g + i] = lw;
+        for (int d = 1; d < kLanes; d <<= 1) {
+#pragma unroll
+          for (int k = 0; k < kTogether; ++k) most[k] = max(most[k], __shfl_xor_sync(0xffffffffu, most[k], d));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+          const int rr = s0 + k * 4 * kRowsAtOnce, row = rr & 127;
+          const uint32_t* u = &v[k].x;
+          // times 2^e the largest lies in (224, 448]; a row with a value that is not finite gets that in its scale, so that its scores have it
+          const int e = most[k] == 0u ? 0 : min(8 - ((int)(most[k] >> 7) - 127) - ((most[k] & 127u) > 96u ? 1 : 0), 126);
+          const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+          if (c == 0) base_ptr[C::ROWEXP + slot * kRows + rr] = most[k] >= 0x7f80u ? 255 : (uint8_t)(127 - e);
+          uint32_t h2[4], l2[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float f0 = __uint_as_float(u[i] << 16) * up, f1 = __uint_as_float(u[i] & 0xffff0000u) * up;
+            h2[i] = __nv_cvt_float2_to_fp8x2(make_float2(f0, f1), __NV_SATFINITE, __NV_E4M3);
+            const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2[i], __NV_E4M3)));
+            l2[i] = __nv_cvt_float2_to_fp8x2(make_float2(f0 - back.x, f1 - back.y), __NV_SATFINITE, __NV_E5M2);
+          }
+          if (c < D / 8) {
+            const uint32_t at = base + C::Q + (rr >> 7) * 2 * C::TILE + C::qchunk(row, c >> 1) + (c & 1) * 8;
+            sts64(at, h2[0] | h2[1] << 16, h2[2] | h2[3] << 16);
+            sts64(at + C::TILE, l2[0] | l2[1] << 16, l2[2] | l2[3] << 16);
           }
         }
-        sts128(hi_at + C::qchunk(t, c), hi[0], hi[1], hi[2], hi[3]);
-        sts128(lo_at + C::qchunk(t, c), lo[0], lo[1], lo[2], lo[3]);
       }
     };
-    auto load = [&](uint32_t row_of_pages) {
-      const uint8_t* src = a.c.v + (size_t)row_of_pages * (kPage * D);
-#pragma unroll
-      for (int p = 0; p < kPasses; ++p) {
-        int row, c;
-        widen_place<D>(p, w, lane, row, c);
-        x[p] = *reinterpret_cast<const uint4*>(src + row * D + c * 16);
+    int nq = 0;                               // items with tiles so far
+    for (int u = 0;; ++u) {
+      const int cs = u % C::NS, vs = u % C::NV;
+      if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_CF + cs), (u / C::NS) & 1, wc, 0))) break;
+      volatile const uint32_t* r = records + cs * 4;
+      const uint32_t f = r[0], m1 = r[1], m2 = r[2];
+      if (!(f & kMore)) break;
+      if (f & kFirst) {
+        if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QR), nq & 1, wc, 0))) break;
+        ++nq;
+        split_q((int)r[3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::B_Q));
       }
-    };
-    auto store = [&](uint32_t to, uint32_t m1, uint32_t m2) {
-#pragma unroll
-      for (int p = 0; p < kPasses; ++p) {
+      if (u >= C::NV && !__all_sync(0xffffffffu, mbar_wait(bar(C::B_VE + vs), ((u / C::NV) - 1) & 1, wc))) break;
+      const uint8_t* from = base_ptr + C::VS0 + cs * C::TILE;
+      const uint32_t to = base + C::V0 + vs * C::VTILE;
+#pragma unroll kUnroll
+      for (int p = 0; p < D / 16; ++p) {
         int row, c;
         widen_place<D>(p, w, lane, row, c);
+        const uint4 x = *reinterpret_cast<const uint4*>(from + C::qchunk(row, c));
+        const uint32_t* in = &x.x;
         uint32_t y[8];
-        const uint32_t* in = &x[p].x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t v = __byte_perm(in[i], 0u, 0x3120);       // bytes 0 1 | 2 3 to where widen_even and widen_odd look
-          y[2 * i] = mul_bf16x2(widen_even(v), m1);
-          y[2 * i + 1] = mul_bf16x2(widen_odd(v), m1);
+          y[2 * i] = mul_bf16x2(widen_even(in[i]), m1);            // bytes 0 and 2: V's columns lie in the order 0 2 1 3 of every
+          y[2 * i + 1] = mul_bf16x2(widen_odd(in[i]), m1);         // four, and so do O's, until it is packed
         }
         if (m2 != kOne2) {
 #pragma unroll
@@ -293,36 +308,14 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       }
       fence_proxy_async_smem();
       __syncwarp();
-    };
-    int nq = 0;
-    for (int u = 0;; ++u) {
-      const int slot = u % kRecords, vs = u % C::NV;
-      if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RF + slot), (u / kRecords) & 1, wc, 0))) break;
-      volatile const uint32_t* r = records + slot * 8;
-      const uint32_t f = r[0], row = r[1], v1 = r[2], v2 = r[3];
-      if (!(f & kMore)) break;
-      if (f & kFirst) {
-        const int is = (int)r[4];
-        if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(bar(C::B_QE), (nq - 1) & 1, wc))) break;   // the item before has taken its last scores
-        ++nq;
-        split_q(items + is * kItemWords, is, 0);
-        split_q(items + is * kItemWords, is, 1);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::B_Q));
-      }
-      load(row);
-      if (lane == 0) mbar_arrive(bar(C::B_RE + slot));
-      if (u >= C::NV && !__all_sync(0xffffffffu, mbar_wait(bar(C::B_VE + vs), ((u / C::NV) - 1) & 1, wc))) break;
-      store(base + C::V0 + vs * C::VTILE, v1, v2);
-      if (lane == 0) mbar_arrive(bar(C::B_VF + vs));
+      if (lane == 0) { mbar_arrive(bar(C::B_CE + cs)); mbar_arrive(bar(C::B_VF + vs)); }
     }
   } else if (warp >= kPagesWarp) {
     RF_REGS_CONTROL();
     if (warp == kPagesWarp) {
       // ------------------------------------------------------------ pages
       int* win = reinterpret_cast<int*>(base_ptr + C::WINDOW);
-      int no = 0, u = 0;                  // items published, tiles published
+      int no = 0, u = 0, nq = 0;          // items published, tiles published, Q fetched
       long long at = st.at;
       int item = st.item;
       bool ok = true;
@@ -330,7 +323,10 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
         if (it.sees < 0) continue;
         const Streams s = streams(a, it);
-        const int n = places(max(s.n0, s.n1)), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+        const int n = max(s.n0, s.n1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
+        at += n + kItemPlaces;
+        pos = min(at, st.hi);
+        if (begin > 0 && begin >= n) continue;            // only the places of the item's end
         int b0, b1, e0, e1;
         if (a.count == nullptr) {       // the streams keep step: they share their tiles
           b0 = min(begin, s.n0); e0 = min(end, s.n0);
@@ -349,8 +345,6 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           mbar_arrive(bar(C::B_IF + slot));
         }
         ++no;
-        at += n;
-        pos = at;
         if (e0 == b0 && e1 == b1) continue;                    // sees nothing, or lists nothing here
         bool first = true;
         const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
@@ -395,37 +389,50 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             if (lane == 0 && first) f |= kFirst;
             const int phys = rf_page(a.c, it.b, min(page, pages - 1), a.dev_status);   // (a page that no row sees: any will do)
             row = (uint32_t)phys * a.c.H + it.bh % a.c.H;
-            prefetch_l2(a.c.v + (size_t)row * (kPage * D), kPage * D);
             vw = rf_cache_attn::widen_by(a.c.v_scale[row]);
           }
-          first = false;
-          // the tiles one after the other, each by the lane that looked it up: V's record, then K
+          // the tiles one after the other, each by the lane that looked it up
           for (int i = 0; i < cnt && ok; ++i, ++u) {
-            const int rs = u % kRecords, ks = u % C::NK;
-            if (u >= kRecords) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0));
-            if (ok && lane == i) {
-              volatile uint32_t* r = records + rs * 8;
-              r[0] = f; r[1] = row; r[2] = vw.m1; r[3] = vw.m2; r[4] = slot;
-              mbar_arrive(bar(C::B_RF + rs));
-            }
-            if (ok && u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0));
+            const int cs = u % C::NS, ks = u % C::NK;
+            if (u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0));
             if (ok && lane == i) {
               flags[ks] = f;
               mbar_expect_tx(bar(C::B_KF + ks), C::TILE);
               tma_load_3d(base + C::K0 + ks * C::TILE, &maps.k, 0, 0, (int)row, bar(C::B_KF + ks));
+            }
+            if (ok && first) {                                     // the item before has taken its last scores: its Q may go
+              if (nq > 0) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QE), (nq - 1) & 1, wc, 0));
+              if (ok && lane == 0) {
+                constexpr uint32_t kBlock = 128 * 128;             // 128 rows of 64 bf16
+                mbar_expect_tx(bar(C::B_QR), 2 * ((D + 63) / 64) * kBlock);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                  for (int kb = 0; kb < (D + 63) / 64; ++kb)
+                    tma_load_3d(base + (D == 64 ? C::RAW : C::Q) + (j * ((D + 63) / 64) + kb) * kBlock, &maps.q, kb * 64, it.r0 + j * BM, it.bh, bar(C::B_QR));
+              }
+              ++nq;
+              first = false;
+            }
+            if (ok && u >= C::NS) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc, 0));
+            if (ok && lane == i) {
+              volatile uint32_t* r = records + cs * 4;
+              r[0] = f; r[1] = vw.m1; r[2] = vw.m2; r[3] = slot;
+              mbar_expect_tx(bar(C::B_CF + cs), C::TILE);
+              tma_load_3d(base + C::VS0 + cs * C::TILE, &maps.v, 0, 0, (int)row, bar(C::B_CF + cs));
             }
           }
           __syncwarp();
         }
       }
       // the end, for the warps that walk tiles and for those that walk items
-      const int rs = u % kRecords, slot = no % kItemSlots, ks = u % C::NK;
+      const int cs = u % C::NS, slot = no % kItemSlots, ks = u % C::NK;
       if (u >= C::NK) mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0);
-      if (u >= kRecords) mbar_wait_long(bar(C::B_RE + rs), ((u / kRecords) - 1) & 1, wc, 0);
+      if (u >= C::NS) mbar_wait_long(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc, 0);
       if (no >= kItemSlots) mbar_wait_long(bar(C::B_IE + slot), ((no / kItemSlots) - 1) & 1, wc, (int)min(st.hi - st.lo, 1ll << 20));
       if (lane == 0) {
-        records[rs * 8] = 0;
-        mbar_arrive(bar(C::B_RF + rs));
+        records[cs * 4] = 0;
+        mbar_arrive(bar(C::B_CF + cs));
         flags[ks] = 0;
         mbar_arrive(bar(C::B_KF + ks));
         items[slot * kItemWords] = -1;
@@ -585,7 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       if (waited > 0) {
         mbar_wait(bar(C::B_Q), nq & 1, wc);
         ++nq;
-        row_scale *= reinterpret_cast<const float*>(base_ptr + C::ROWSCALE)[slot * kRows + j * BM + row_in_tile];
+        const uint32_t e = base_ptr[C::ROWEXP + slot * kRows + j * BM + row_in_tile];
+        row_scale *= __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
       }
       bool opens = true;
       for (int t = begin; t < end; ++t, ++done, opens = false) {
@@ -751,7 +759,12 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           }
           if (there) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+            for (int i = 0; i < 8; ++i) {                  // columns 0 2 1 3 of every four
+              const float x0 = __uint_as_float(v[4 * i]) * inv, x2 = __uint_as_float(v[4 * i + 1]) * inv;
+              const float x1 = __uint_as_float(v[4 * i + 2]) * inv, x3 = __uint_as_float(v[4 * i + 3]) * inv;
+              v[2 * i] = pack_bf16(x0, x1);
+              v[2 * i + 1] = pack_bf16(x2, x3);
+            }
             store_columns(o + c * 4, v, o32);
           }
         }
@@ -819,8 +832,8 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   uint32_t v[8];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    v[2 * k] = pack_bf16(acc[k].x * inv, acc[k].y * inv);
-    v[2 * k + 1] = pack_bf16(acc[k].z * inv, acc[k].w * inv);
+    v[2 * k] = pack_bf16(acc[k].x * inv, acc[k].z * inv);        // columns 0 2 1 3 of every four
+    v[2 * k + 1] = pack_bf16(acc[k].y * inv, acc[k].w * inv);
   }
   const size_t at_row = (size_t)it.bh * a.u.rows + row;
   store_sector(reinterpret_cast<uint4*>(a.o + at_row * D) + c0 / 2, v, (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0);
@@ -848,7 +861,9 @@ rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
     configured[dev] = true;
   }
   Maps maps;
-  if (!rf_encode_pages_map(&maps.k, a.c.k, a.c)) return RF_ERR_CUDA;
+  if (!rf_encode_rows_map(&maps.q, a.u.q, D, a.u.rows, (size_t)D * 2, (size_t)a.u.rows * D * 2, a.c.B * a.c.H) || !rf_encode_pages_map(&maps.k, a.c.k, a.c) ||
+      !rf_encode_pages_map(&maps.v, a.c.v, a.c))
+    return RF_ERR_CUDA;
   const int ctas = chunk_ctas(a.c, a.u);
   if (rf_launch(rf_cache_chunk_kernel<D, LSE>, dim3(ctas), kThreads, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
   if (ctas == 1) return RF_OK;
