@@ -163,14 +163,30 @@ __device__ __forceinline__ int code_units(uint32_t code) {
   const int v = e == 0 ? m : (8 + m) << (e - 1);
   return code & 0x80 ? -v : v;
 }
-__device__ __forceinline__ float code_value(uint32_t code) { return (float)code_units(code) * 0.001953125f; }
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
-// One page of one head, K or V.  A thread takes 8 columns (16 bytes in, 8 out) of every 16th row, all loads first; the page's
-// largest magnitude has to be known before the first code, so a page is held in registers and read once.  Bound by HBM for
-// whole frames (6 bytes a pair of values of K and V); for single tokens by the two launches.  The page's old tokens are
-// read and written again only where they move to another page or another scale; K's are read for the sum.
-// The sum of the codes is taken in integers, so it is the same however the page was filled.
+// Eight codes of a row.
+__device__ __forceinline__ uint2 encode8(const float (&f)[8]) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(make_float2(f[2 * i], f[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+}
+__device__ __forceinline__ void decode8(uint2 code, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i < 2 ? code.x : code.y) >> (16 * (i & 1))), __NV_E4M3)));
+    f[2 * i] = x.x;
+    f[2 * i + 1] = x.y;
+  }
+}
+
+// One page of one head, K or V.  A thread takes 8 columns (16 bytes in, 8 out) of every 16th row, all loads first; the new tokens'
+// largest magnitude has to be known before the first code, so they are held in registers and read once.  Bound by HBM for
+// whole frames (6 bytes a pair of values of K and V); for single tokens by the two launches.  The page's old tokens, in a sequence's first
+// page, are gone through in a loop of their own: written again only where they move to another page or another scale, K's read for the sum.
+// The sum of the codes does not depend on how the page was filled: a thread's eight rows are exact in fp32 (multiples of 2^-9 below 2^12),
+// and the threads' sums are added as integers.
 template <int D>
 __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const __nv_bfloat16* kx, const __nv_bfloat16* vx, int M, const int32_t* ws,
                                                                int32_t* dev_status) {
@@ -182,10 +198,8 @@ __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const 
   const PlanWs w = plan_ws(const_cast<int32_t*>(ws), c.B, c.n_pages);
   rf_grid_trigger();
   rf_grid_wait();
-  const int add = w.n_new[b];
-  if (add == 0) return;
-  const int len = w.old_len[b], page = len / kPage + blockIdx.x, t0 = page * kPage;
-  if (t0 >= len + add) return;
+  const int add = w.n_new[b], len = w.old_len[b], page = len / kPage + blockIdx.x, t0 = page * kPage;
+  if (add == 0 || t0 >= len + add) return;
   const int held = max(0, min(kPage, len - t0)), end = min(kPage, len + add - t0);
   const int dst = c.table[(size_t)b * c.max_pages + page];
   if (!rf_in_bounds(dst, c.n_pages, dev_status)) return;
@@ -195,102 +209,93 @@ __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const 
   const __nv_bfloat16* x = (keys ? kx : vx) + (((size_t)b * c.H + h) * M + (t0 - len)) * D + col * 8;
   const size_t block = (size_t)kPage * D;
   uint8_t* data = keys ? c.k : c.v;
-  const uint8_t* old = data + ((size_t)src * c.H + h) * block + col * 8;
   uint8_t* out = data + ((size_t)dst * c.H + h) * block + col * 8;
   float* scales = keys ? c.k_scale : c.v_scale;
-  const uint32_t old_bits = held ? __float_as_uint(scales[(size_t)src * c.H + h]) : 0u;
+  const int e_old = held ? min(max((int)(__float_as_uint(scales[(size_t)src * c.H + h]) >> 23) - 127, -100), 100) : -100;
   uint4 v[kPasses];
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     const int r = row0 + 16 * p;
-    v[p] = make_uint4(0u, 0u, 0u, 0u);
-    if (r < held) {
-      const uint2 t = *reinterpret_cast<const uint2*>(old + (size_t)r * D);
-      v[p].x = t.x; v[p].y = t.y;
-    } else if (r < end) {
-      v[p] = *reinterpret_cast<const uint4*>(x + (size_t)r * D);
-    }
+    v[p] = r >= held && r < end ? *reinterpret_cast<const uint4*>(x + (size_t)r * D) : make_uint4(0u, 0u, 0u, 0u);
   }
   // largest finite magnitude of the new tokens, as bf16 bits
   uint32_t most = 0u;
-  bool odd = false;
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
-    const int r = row0 + 16 * p;
-    if (r < held || r >= end) continue;
     const uint32_t* u = &v[p].x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
-      const bool flo = lo < 0x7f80u, fhi = hi < 0x7f80u;
-      odd |= !flo | !fhi;
-      most = max(most, max(flo ? lo : 0u, fhi ? hi : 0u));
+    for (int i = 0; i < 4; ++i) most = max(most, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+  }
+  if (most >= 0x7f80u) {                                     // something is not finite: NaN becomes zero, infinities saturate
+    rf_report(dev_status, RF_ERR_NOT_FINITE);
+    most = 0u;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      uint32_t* u = &v[p].x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((u[i] & 0x7fffu) > 0x7f80u) u[i] &= 0xffff0000u;
+        if (((u[i] >> 16) & 0x7fffu) > 0x7f80u) u[i] &= 0xffffu;
+        const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
+        most = max(most, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+      }
     }
   }
-  if (odd) rf_report(dev_status, RF_ERR_NOT_FINITE);
   most = __reduce_max_sync(0xffffffffu, most);
   if ((tid & 31) == 0) red[tid >> 5] = (int)most;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) most = max(most, (uint32_t)red[i]);
   // 448 = 1.75 * 2^8, so with m * 2^E the largest magnitude e is E - 8, or E - 7 where m > 1.75; subnormal ones end at -100
-  int e = (int)(most >> 7) - 127 - ((most & 127u) > 96u ? 7 : 8);
-  e = min(max(e, -100), 100);
-  const int e_old = (int)(old_bits >> 23) - 127;
-  const bool moves = held && (src != dst || e > e_old);    // old tokens get another place or scale
-  const int e_new = held ? max(e, min(max(e_old, -100), 100)) : e;
-  const float inv = pow2f(-e_new);
-  const float again = held ? pow2f(max(min(max(e_old, -100), 100) - e_new, -126)) : 1.f;
-  int acc[8] = {};
+  const int e = min(max(max((int)(most >> 7) - 127 - ((most & 127u) > 96u ? 7 : 8), e_old), -100), 100);
+  const float inv = pow2f(-e);
+  float acc[8] = {};
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
     const int r = row0 + 16 * p;
-    if (r >= end) continue;
-    uint2 code;
-    if (r < held) {
-      code = make_uint2(v[p].x, v[p].y);
-      if (again != 1.f) {
-        uint32_t* cw = &code.x;
+    if (r < held || r >= end) continue;
+    float f[8];
+    const uint32_t* u = &v[p].x;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t t = cw[i];
-          const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(code_value(t & 255u) * again, code_value((t >> 8) & 255u) * again), __NV_SATFINITE, __NV_E4M3);
-          const uint32_t z = __nv_cvt_float2_to_fp8x2(make_float2(code_value((t >> 16) & 255u) * again, code_value(t >> 24) * again), __NV_SATFINITE, __NV_E4M3);
-          cw[i] = a | (z << 16);
-        }
-      }
-    } else {
-      uint32_t* cw = &code.x;
-      const uint32_t* u = &v[p].x;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float f[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t half = j & 1 ? u[2 * i + j / 2] & 0xffff0000u : u[2 * i + j / 2] << 16;
-          f[j] = (half & 0x7fffffffu) > 0x7f800000u ? 0.f : __uint_as_float(half) * inv;   // NaN -> 0; infinities saturate
-        }
-        const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t z = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
-        cw[i] = a | (z << 16);
-      }
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(u[i] << 16) * inv;
+      f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u) * inv;
     }
-    if (r >= held || moves) *reinterpret_cast<uint2*>(out + (size_t)r * D) = code;
+    const uint2 code = encode8(f);
+    *reinterpret_cast<uint2*>(out + (size_t)r * D) = code;
     if (keys) {
+      decode8(code, f);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        acc[i] += code_units((code.x >> (8 * i)) & 255u);
-        acc[4 + i] += code_units((code.y >> (8 * i)) & 255u);
+      for (int i = 0; i < 8; ++i) acc[i] += f[i];
+    }
+  }
+  const bool moves = src != dst || e > e_old;                // old tokens get another place or scale
+  if (held && (keys || moves)) {
+    const uint8_t* old = data + ((size_t)src * c.H + h) * block + col * 8;
+    const float again = pow2f(max(e_old - e, -126));
+#pragma unroll 4
+    for (int r = row0; r < held; r += 16) {
+      uint2 code = *reinterpret_cast<const uint2*>(old + (size_t)r * D);
+      float f[8];
+      decode8(code, f);
+      if (e > e_old) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= again;
+        code = encode8(f);
+        decode8(code, f);
       }
+      if (moves) *reinterpret_cast<uint2*>(out + (size_t)r * D) = code;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += f[i];
     }
   }
   const size_t side = (size_t)dst * c.H + h;
-  if (tid == 0) scales[side] = pow2f(e_new);
+  if (tid == 0) scales[side] = pow2f(e);
   if (!keys) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) atomicAdd(&sums[col * 8 + i], acc[i]);
+  for (int i = 0; i < 8; ++i) atomicAdd(&sums[col * 8 + i], __float2int_rn(acc[i] * 512.f));
   __syncthreads();
-  if (tid < D) c.k_sum[side * D + tid] = (float)sums[tid] * 0.001953125f * pow2f(e_new);
+  if (tid < D) c.k_sum[side * D + tid] = (float)sums[tid] * 0.001953125f * pow2f(e);
 }
 
 // ------------------------------------------------------------------------------------------------ fork, drop
@@ -455,10 +460,12 @@ __global__ void __launch_bounds__(256) rf_cache_move_kernel(RfCache c, const int
 }
 
 // ------------------------------------------------------------------------------------------------ select
-// One CTA per tile of query rows: their sum, its product with every page's key sum, the top_k best, the list in order.
-// Scores are in 64 bits: a page's place must not hang on the order of a summation, and two scores that differ in exact
-// arithmetic hardly ever agree to 1e-16.  The key sums of a head (n_pages * D floats) are read by every tile, from the L2.
-constexpr int kSelThreads = 256;
+// A CTA takes up to 8 tiles of query rows of a K/V head: their sums, their products with every page's key sum, the top_k best of each,
+// the lists in order.  Scores are in 64 bits: a page's place must not hang on the order of a summation, and two scores that differ in
+// exact arithmetic hardly ever agree to 1e-16.  What bounds it: widening the key sums to 64 bits (16 a cycle and SM), so a lane takes a
+// page, widens its D numbers once and multiplies them with all of the CTA's tiles; a tile's own pass per CTA was 136 us for 29
+// tiles x 931 pages x 24 heads, 83 us for a token each of 32 heads.
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 
 __device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below everything
   if (isnan(x)) return 0ull;
@@ -466,113 +473,125 @@ __device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below
   return u >> 63 ? ~u : u | (1ull << 63);
 }
 
-template <int D>
+template <int D, int T>
 __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c, RfQueries u, int keep_first, int keep_last, int top_k, int32_t* count,
                                                                       int32_t* pages, int n_k, int32_t* dev_status) {
-  constexpr int kCols = D / 8, kGroups = kSelThreads / kCols, kPer = D / 32;
-  extern __shared__ uint64_t key[];                       // [pages of the sequence]
-  __shared__ double part[kGroups][D];
-  __shared__ double pooled[D];
-  __shared__ float tail_sum[D];
-  __shared__ int hist[256], state[4], warp_n[kSelThreads / 32][2];
+  constexpr int kOf = kSelWarps / T, kTeam = 32 * kOf;     // warps and threads that work on a tile
+  extern __shared__ uint64_t keys[];                       // [T][pages of the sequence]
+  __shared__ double part[kSelWarps][D];
+  __shared__ __align__(16) double pooled[D][T];
+  __shared__ __align__(16) float tail_sum[D];
+  __shared__ int hist[T][256], state[T][4], warp_n[kSelWarps][2], cand[T + 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int mine = warp / kOf, rank = tid % kTeam, wrank = warp % kOf;     // this thread's tile, and its place in the tile's team
+  const int tile = blockIdx.x * T + mine, h = blockIdx.y, b = blockIdx.z;
   rf_grid_trigger();
   rf_grid_wait();
   const int len = rf_seq_len(c, b, dev_status), q_len = rf_query_len(u, b, dev_status);
-  const int sees = rf_rows_see(u, len, q_len, tile * kPage, kPage);
-  const size_t row = ((size_t)b * c.H + h) * u.n_q + tile;
-  const int n = min(rf_pages(max(sees, 0)), kSelectMaxPages);
-  if (n == 0) {
-    if (tid == 0) count[row] = 0;
-    return;
-  }
+  const int sees = tile < u.n_q ? rf_rows_see(u, len, q_len, tile * kPage, kPage) : -1;
+  const size_t row = ((size_t)b * c.H + h) * u.n_q + min(tile, u.n_q - 1);
+  const int n = min(rf_pages(max(sees, 0)), kSelectMaxPages);             // pages in which some row of the tile sees a key
   const int first_end = min(keep_first, n), last_begin = max(n - min(keep_last, n), first_end);
   const int rest = last_begin - first_end, best = min(top_k, rest);
+  const bool scored = best > 0 && best < rest;
+  if (rank == 0) cand[mine] = scored ? last_begin : 0;
+  if (tid == 0) cand[T] = 0;
+  __syncthreads();
+  if (rank == 0 && scored) atomicMax(&cand[T], last_begin);
+  __syncthreads();
+  const int most = cand[T];                                 // pages to be scored: [keep_first, most)
   uint64_t threshold = ~0ull;
-  int equal_allowed = 0;                                  // pages of exactly the threshold's score that are taken, lowest first
-  if (best > 0 && best < rest) {
+  int equal_allowed = 0;                                    // pages of exactly the threshold's score that are taken, lowest first
+  if (most > 0) {                                           // (the same for the whole CTA)
     {
-      const int col = tid % kCols, group = tid / kCols;
-      if (group < kGroups) {
-        double acc[8] = {};
-        const __nv_bfloat16* q = u.q + (((size_t)b * c.H + h) * u.rows) * D + col * 8;
-        for (int r = group; r < kPage; r += kGroups) {
-          const int at = tile * kPage + r;
-          if (at >= u.rows) break;
-          if (at % u.M >= q_len) continue;
-          const uint4 v = *reinterpret_cast<const uint4*>(q + (size_t)at * D);
-          const uint32_t* x = &v.x;
+      // the sums of the tile's rows, a lane every 32nd column, a warp every kOf-th row
+      double acc[D / 32] = {};
+      const __nv_bfloat16* q = u.q + (((size_t)b * c.H + h) * u.rows + (size_t)tile * kPage) * D + lane;
+      const int rows = scored ? min(kPage, u.rows - tile * kPage) : 0;
+#pragma unroll 4
+      for (int r = wrank; r < rows; r += kOf) {
+        const int at = tile * kPage + r;
+        if ((u.G == 1 ? at : at % u.M) >= q_len) continue;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[2 * i] += (double)__uint_as_float(x[i] << 16);
-            acc[2 * i + 1] += (double)__uint_as_float(x[i] & 0xffff0000u);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) part[group][col * 8 + i] = acc[i];
+        for (int i = 0; i < D / 32; ++i) acc[i] += (double)__bfloat162float(q[(size_t)r * D + 32 * i]);
       }
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) part[warp][lane + 32 * i] = acc[i];
     }
-    __syncthreads();
-    if (tid < D) {
-      double s = 0.0;
-      for (int g = 0; g < kGroups; ++g) s += part[g][tid];
-      pooled[tid] = s;
-    }
-    __syncthreads();
     // A last page that is not full is summed up from its codes: it may be part of a page that another sequence has filled
     // further, or that was fuller when it was written.
-    const int tail = len % kPage != 0 && last_begin == rf_pages(len) ? last_begin - 1 : -1;
-    if (tail >= 0) {
+    const int tail = len % kPage != 0 && most == rf_pages(len) ? most - 1 : -1;
+    if (tail >= 0 && tid < D) {
       const size_t side = (size_t)rf_page(c, b, tail, dev_status) * c.H + h;
-      const uint8_t* codes = c.k + side * kPage * D;
-      if (tid < D) {
-        int sum = 0;
-        for (int r = 0; r < len % kPage; ++r) sum += code_units(codes[r * D + tid]);
-        tail_sum[tid] = (float)sum * 0.001953125f * c.k_scale[side];
-      }
-      __syncthreads();
+      const uint8_t* codes = c.k + side * kPage * D + tid;
+      int sum = 0;
+#pragma unroll 8
+      for (int r = 0; r < len % kPage; ++r) sum += code_units(codes[r * D]);
+      tail_sum[tid] = (float)sum * 0.001953125f * c.k_scale[side];
     }
-    double p[kPer];
+    __syncthreads();
+    for (int i = tid; i < T * D; i += kSelThreads) {
+      const int t = i / D, d = i % D;
+      double x = 0.0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) p[i] = pooled[lane + 32 * i];
-    constexpr int kAhead = 4;                              // pages of a warp under way together
-    for (int c0 = first_end + warp; c0 < last_begin; c0 += kAhead * 8) {
-      float s[kAhead][kPer];
+      for (int k = 0; k < kOf; ++k) x += part[t * kOf + k][d];
+      pooled[d][t] = x;
+    }
+    __syncthreads();
+    for (int c0 = keep_first + warp * 32; c0 < most; c0 += kSelThreads) {
+      const int col = c0 + lane;
+      const bool there = col < most;
+      const float4* x = reinterpret_cast<const float4*>(col == tail ? tail_sum : c.k_sum + ((size_t)(there ? rf_page(c, b, col, dev_status) : 0) * c.H + h) * D);
+      double dot[T] = {};
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        const float4 v = there ? x[d / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int col = c0 + 8 * j;
-        const float* x = c.k_sum + ((size_t)(col < last_begin ? rf_page(c, b, col, dev_status) : 0) * c.H + h) * D + lane;
+        for (int k = 0; k < 4; ++k) {
+          const double w = (double)f[k];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) s[j][i] = col == tail ? tail_sum[lane + 32 * i] : x[32 * i];
+          for (int t = 0; t < T; ++t) dot[t] += pooled[d + k][t] * w;
+        }
       }
+      if (there) {
+        const double tokens = (double)min(kPage, len - col * kPage);
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int col = c0 + 8 * j;
-        double d = 0.0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) d += p[i] * (double)s[j][i];
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) d += __shfl_xor_sync(0xffffffffu, d, x);
-        if (lane == 0 && col < last_begin) key[col] = ordered(d / (double)min(kPage, len - col * kPage));
+        for (int t = 0; t < T; ++t)
+          if (col < cand[t]) keys[(size_t)t * c.max_pages + col] = ordered(dot[t] / tokens);
       }
     }
+    __syncthreads();
+  }
+  // From here on every tile's team works by itself.
+  auto team_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "n"(kTeam) : "memory"); };
+  const uint64_t* key = keys + (size_t)mine * c.max_pages;
+  if (scored) {
     // the best-th largest: eight bits at a time
     uint64_t prefix = 0ull;
     int need = best;
     for (int shift = 56; shift >= 0; shift -= 8) {
-      hist[tid] = 0;
-      __syncthreads();
-      for (int i = first_end + tid; i < last_begin; i += kSelThreads) {
-        const uint64_t k = key[i];
-        if (shift == 56 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(int)(k >> shift) & 255], 1);
+      for (int i = rank; i < 256; i += kTeam) hist[mine][i] = 0;
+      team_sync();
+      for (int base = first_end + wrank * 32; base < last_begin; base += kTeam) {
+        const int i = base + lane;
+        const uint64_t k = i < last_begin ? key[i] : 0ull;
+        const bool in = i < last_begin && (shift == 56 || (k >> (shift + 8)) == prefix);
+        const int bin = in ? (int)(k >> shift) & 255 : -1;
+        int same;                                           // the leading digits are alike: one addition for the warp
+        __match_all_sync(0xffffffffu, bin, &same);
+        if (same) {
+          if (in && lane == 0) atomicAdd(&hist[mine][bin], 32);
+        } else if (in) {
+          atomicAdd(&hist[mine][bin], 1);
+        }
       }
-      __syncthreads();
-      if (warp == 0) {                                     // from the top bin down: where `need` is reached
+      team_sync();
+      if (wrank == 0) {                                     // from the top bin down: where `need` is reached
         int v[8], sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          v[i] = hist[255 - (lane * 8 + i)];
+          v[i] = hist[mine][255 - (lane * 8 + i)];
           sum += v[i];
         }
         int before = sum;
@@ -586,36 +605,31 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             if (before < need && before + v[i] >= need) {
-              state[0] = 255 - (lane * 8 + i);
-              state[1] = need - before;
-              state[2] = v[i];
+              state[mine][0] = 255 - (lane * 8 + i);
+              state[mine][1] = need - before;
+              state[mine][2] = v[i];
               break;
             }
             before += v[i];
           }
         }
       }
-      __syncthreads();
-      prefix = prefix << 8 | (uint64_t)state[0];
-      need = state[1];
-      const int in_bin = state[2];
+      team_sync();
+      prefix = prefix << 8 | (uint64_t)state[mine][0];
+      need = state[mine][1];
+      const int in_bin = state[mine][2];
       threshold = prefix << shift;
       equal_allowed = need;
-      __syncthreads();
-      if (in_bin == need) {                                // the whole bin is taken: everything from its lower end on
+      if (in_bin == need) {                                 // the whole bin is taken: everything from its lower end on
         equal_allowed = 0x7fffffff;
         break;
       }
     }
-  } else if (best == rest) {
-    threshold = 0ull;
-    equal_allowed = 0x7fffffff;
   }
   // the list, in order
-  const bool scored = best > 0 && best < rest;
   int out = 0, ties = 0;
-  for (int base = 0; base < n; base += kSelThreads) {
-    const int col = base + tid;
+  for (int base = 0; base < n; base += kTeam) {
+    const int col = base + rank;
     const bool always = col < n && (col < first_end || col >= last_begin);
     const bool candidate = col < n && !always && best > 0;
     const uint64_t k = candidate && scored ? key[col] : 0ull;
@@ -623,30 +637,30 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
     const bool tie = candidate && scored && equal_allowed != 0x7fffffff && k == threshold;
     const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
     if (lane == 0) warp_n[warp][0] = __popc(tie_mask);
-    __syncthreads();
+    team_sync();
     int tie_rank = ties + __popc(tie_mask & ((1u << lane) - 1u)), tie_all = 0;
 #pragma unroll
-    for (int i = 0; i < kSelThreads / 32; ++i) {
-      if (i < warp) tie_rank += warp_n[i][0];
-      tie_all += warp_n[i][0];
+    for (int i = 0; i < kOf; ++i) {
+      if (i < wrank) tie_rank += warp_n[mine * kOf + i][0];
+      tie_all += warp_n[mine * kOf + i][0];
     }
     bool take = always;
     if (candidate) take = !scored ? true : tie ? tie_rank < equal_allowed : equal_allowed == 0x7fffffff ? k >= threshold : k > threshold;
     const uint32_t mask = __ballot_sync(0xffffffffu, take);
     if (lane == 0) warp_n[warp][1] = __popc(mask);
-    __syncthreads();
+    team_sync();
     int at = out + __popc(mask & ((1u << lane) - 1u)), all = 0;
 #pragma unroll
-    for (int i = 0; i < kSelThreads / 32; ++i) {
-      if (i < warp) at += warp_n[i][1];
-      all += warp_n[i][1];
+    for (int i = 0; i < kOf; ++i) {
+      if (i < wrank) at += warp_n[mine * kOf + i][1];
+      all += warp_n[mine * kOf + i][1];
     }
     if (take && at < n_k && rf_in_bounds(at, n_k, dev_status)) pages[row * n_k + at] = col;
     out += all;
     ties += tie_all;
-    __syncthreads();
+    team_sync();
   }
-  if (tid == 0) count[row] = min(out, n_k);
+  if (rank == 0 && tile < u.n_q) count[row] = min(out, n_k);
 }
 
 template <typename K>
@@ -654,7 +668,7 @@ cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess || bytes <= 48 * 1024 || (dev < 64 && done[dev])) return e;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024);
   if (e == cudaSuccess && dev < 64) done[dev] = true;
   return e;
 }
@@ -705,17 +719,19 @@ cudaError_t rf_launch_cache_compact(const RfCache& c, int32_t* n_live, int32_t* 
 
 cudaError_t rf_launch_cache_select(const RfCache& c, const RfQueries& u, int keep_first, int keep_last, int top_k, int32_t* count,
                                    int32_t* pages, int n_k, int32_t* dev_status, cudaStream_t st) {
-  const size_t smem = sizeof(uint64_t) * (size_t)c.max_pages;
-  const dim3 grid(u.n_q, c.H, c.B);
+  // Four tiles a CTA share the widening of the key sums; one where the scores of four do not fit in shared memory or there are no
+  // four tiles.
+  const bool four = u.n_q >= 4 && 4 * sizeof(uint64_t) * (size_t)c.max_pages <= 128 * 1024;
+  const size_t smem = (four ? 4 : 1) * sizeof(uint64_t) * (size_t)c.max_pages;
   auto go = [&](auto kernel, bool (&done)[64]) -> cudaError_t {
-    const cudaError_t e = allow_smem(kernel, smem + 32 * 1024, done);   // (the static arrays count too)
+    const cudaError_t e = allow_smem(kernel, smem + 48 * 1024, done);   // (the static arrays count too)
     if (e != cudaSuccess) return e;
-    return rf_launch(kernel, grid, kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
+    return rf_launch(kernel, dim3(rf_cdiv(u.n_q, four ? 4 : 1), c.H, c.B), kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
   };
-  static bool d64[64] = {}, d96[64] = {}, d128[64] = {};
+  static bool done[6][64] = {};
   switch (c.D) {
-    case 64: return go(rf_cache_select_kernel<64>, d64);
-    case 96: return go(rf_cache_select_kernel<96>, d96);
-    default: return go(rf_cache_select_kernel<128>, d128);
+    case 64: return four ? go(rf_cache_select_kernel<64, 4>, done[0]) : go(rf_cache_select_kernel<64, 1>, done[1]);
+    case 96: return four ? go(rf_cache_select_kernel<96, 4>, done[2]) : go(rf_cache_select_kernel<96, 1>, done[3]);
+    default: return four ? go(rf_cache_select_kernel<128, 4>, done[4]) : go(rf_cache_select_kernel<128, 1>, done[5]);
   }
 }

@@ -2,11 +2,14 @@
 //
 // o = softmax(scale q k^T) v, over the keys that each row sees.  Every K and V byte is used by at most 16 rows, so the floor is
 // the cache's bytes at the HBM rate: an SM has 1400 cycles for the 32 KB of a tile of 128 keys at D = 128.
-// A producer warp streams the tiles into a ring in shared memory by TMA (page by page, swizzled, 128 KB under way); eight warps
-// take 16 keys of a tile each: S = q K^T and O += P V on mma.sync (16 rows x 8 keys x 16; the tensor pipe idles at any rate here,
-// and a tcgen05 tile is 128 rows), codes widened to bf16 in registers, exactly.  The order of a contraction is free, so the
-// words are used as they lie: K's four bytes of a word are four of the 16 terms of one instruction, and V's bytes of two
-// keys are brought together by one byte permutation.  Each warp keeps its own maxima and sums (fp32); they meet once per item.
+// A producer warp streams the tiles into rings in shared memory by TMA (page by page, swizzled, 128 KB under way).  Eight warps
+// take 16 keys of a tile each, on mma.sync with the keys as its 16 rows and the queries as its 8 columns (tcgen05 would spend 128 rows on
+// them): S^T = K q^T, then O^T += V^T P^T with P^T turned round by movmatrix.  Codes are widened to bf16 in registers, exactly.  The order
+// of a contraction is free, so the words are used as they lie: a word of K is four of the 16 terms of one instruction, and V's bytes
+// of two keys are brought together by one byte permutation.  Up to 8 rows, two groups of eight warps take the tiles in turn, four warps
+// to a scheduler (one group, and queries as rows of the product: 190 us for 33 frames of 3600 tokens, 24 heads, where the bytes take 112);
+// 9 to 16 rows have two column blocks, which share the widened words, and one group, for its registers.
+// Each warp keeps its own maxima and sums (fp32); they meet once per item.
 #include <algorithm>
 
 #include "rf_cache_attn.cuh"
@@ -16,23 +19,23 @@ using namespace rf_cache_attn;
 
 namespace {
 
-constexpr int kRows = 16, kWarps = 8, kThreads = 32 * (kWarps + 1);
 enum { kFirst = 1, kLast = 2, kNothing = 4, kHeadPiece = 8, kTailPiece = 16, kEnd = 32 };
 
-template <int D>
+template <int D, int NB>
 struct Cfg {
+  static constexpr int ROWS = 8 * NB, GROUPS = NB == 1 ? 2 : 1, WARPS = 8 * GROUPS, THREADS = 32 * (WARPS + 1);
   static constexpr int PITCH = D == 64 ? 64 : 128;                  // bytes of a row in shared memory
   static constexpr uint32_t TILE = kPage * PITCH;
-  static constexpr int STAGES = D == 64 ? 8 : 4;
-  static constexpr uint32_t JOIN = STAGES * 2 * TILE;               // [kWarps][kRows][D] float
-  static constexpr uint32_t SUMS = JOIN + kWarps * kRows * D * 4;   // [kWarps][kRows] {m, l, l of the unrounded weights}
-  static constexpr uint32_t BAR = SUMS + kWarps * kRows * 16;
-  static constexpr uint32_t REC = BAR + 8 * (2 * STAGES + 2);
-  static constexpr uint32_t MISC = REC + STAGES * 32;
+  static constexpr int SLOTS = D == 64 ? 8 : 4, STAGES = SLOTS / GROUPS;   // slots in all; of a group's ring
+  static constexpr uint32_t JOIN = SLOTS * 2 * TILE;                // [WARPS][ROWS][D] float
+  static constexpr uint32_t SUMS = JOIN + WARPS * ROWS * D * 4;     // [WARPS][ROWS] {m, l, l of the unrounded weights}
+  static constexpr uint32_t BAR = SUMS + WARPS * ROWS * 16;
+  static constexpr uint32_t REC = BAR + 8 * (2 * SLOTS + 2);
+  static constexpr uint32_t MISC = REC + SLOTS * 32;
   static constexpr uint32_t TOTAL = MISC + 16 + sizeof(StretchScratch);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
-  static constexpr int PIECE = kRows * (D + 4);                     // floats: O [kRows][D], then {m, l, l exact, 0} per row
+  static constexpr int PIECE = ROWS * (D + 4);                      // floats: O [ROWS][D], then {m, l, l exact, 0} per row
   // byte offset of 16-byte chunk c of row r
   static __device__ __forceinline__ uint32_t chunk(int r, int c) {
     return r * PITCH + ((D == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4);
@@ -53,12 +56,18 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+  return d;
+}
 
 // Key tiles that an item walks; -1: all of its rows are padding.
 __device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem& it) {
   if (it.sees < 0) return -1;
   return a.count == nullptr ? rf_pages(it.sees) : listed(a, it, it.r0 / kPage);
 }
+template <int kRows>
 struct TokenPlaces {
   static constexpr int kRowsOf = kRows, kEnd = 2;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
   static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
@@ -69,21 +78,22 @@ struct TokenPlaces {
 
 struct Maps { CUtensorMap k, v; };
 
-template <int D, bool LSE>
-__global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
-  using C = Cfg<D>;
+template <int D, int NB, bool LSE>
+__global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
+  using C = Cfg<D, NB>;
+  constexpr int kRows = C::ROWS, kWarps = C::WARPS;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
   auto full = [&](int s) -> uint32_t { return base + C::BAR + 8u * s; };
-  auto empty = [&](int s) -> uint32_t { return base + C::BAR + 8u * (C::STAGES + s); };
-  const uint32_t joined = base + C::BAR + 8u * (2 * C::STAGES), read = joined + 8;   // all pieces of an item are in shared memory; they have been read
+  auto empty = [&](int s) -> uint32_t { return base + C::BAR + 8u * (C::SLOTS + s); };
+  const uint32_t joined = base + C::BAR + 8u * (2 * C::SLOTS), read = joined + 8;   // all warps' rows of an item are in shared memory; they have been read
   volatile Record* records = reinterpret_cast<volatile Record*>(base_ptr + C::REC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC);
   StretchScratch* scratch = reinterpret_cast<StretchScratch*>(base_ptr + C::MISC + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
-    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kWarps); }
+    for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 8); }
     mbar_init(joined, kWarps);
     mbar_init(read, kWarps);
     *abort_flag = 0;
@@ -92,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
   if (tid == 32 * kWarps) { prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
   rf_grid_trigger();
   rf_grid_wait();
-  const Stretch st = stretch<TokenPlaces, kThreads>(a, scratch);      // (its barriers also publish the mbarriers)
+  const Stretch st = stretch<TokenPlaces<kRows>, C::THREADS>(a, scratch);      // (its barriers also publish the mbarriers)
   const WaitCtx wc{abort_flag, a.dev_status};
   if (tid == 0) {
     int32_t* head = reinterpret_cast<int32_t*>(a.ws) + blockIdx.x * kHeadWords;
@@ -101,46 +111,44 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
   }
 
   if (warp == kWarps) {
-    // ------------------------------------------------------------ producer
-    int stage = 0, item = st.item;
-    uint32_t phase = 1;                       // of the empty barriers: the first round finds them free
+    // ------------------------------------------------------------ producer: tile t of a piece goes to group t mod GROUPS
+    int sent[C::GROUPS] = {}, item = st.item;
     long long at = st.at;
-    auto publish = [&](const Record& r, bool bytes, int row) {   // lane 0
-      if (!mbar_wait(empty(stage), phase, wc)) return;            // abandoned: nothing more is fetched
-      volatile Record* d = records + stage;
+    auto publish = [&](const Record& r, int group, bool bytes, int row) {   // lane 0
+      const int n = sent[group], s = group * C::STAGES + n % C::STAGES;
+      if (!mbar_wait(empty(s), ((n / C::STAGES) & 1) ^ 1, wc)) return;        // (the first round finds them free) abandoned: nothing more is fetched
+      volatile Record* d = records + s;
       d->item = r.item; d->page = r.page; d->flags = r.flags;
       d->k1 = r.k1; d->k2 = r.k2; d->v1 = r.v1; d->v2 = r.v2;
       if (bytes) {
-        const uint32_t to = base + stage * 2 * C::TILE;
-        mbar_expect_tx(full(stage), 2 * C::TILE);
-        tma_load_3d(to, &maps.k, 0, 0, row, full(stage));
-        tma_load_3d(to + C::TILE, &maps.v, 0, 0, row, full(stage));
+        const uint32_t to = base + s * 2 * C::TILE;
+        mbar_expect_tx(full(s), 2 * C::TILE);
+        tma_load_3d(to, &maps.k, 0, 0, row, full(s));
+        tma_load_3d(to + C::TILE, &maps.v, 0, 0, row, full(s));
       } else {
-        mbar_arrive(full(stage));
+        mbar_arrive(full(s));
       }
-    };
-    auto step = [&]() {
-      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
     };
     for (long long pos = st.lo; pos < st.hi; ++item) {
       const CacheItem it = cache_item<kRows>(a, item);
       const int tiles = item_tiles(a, it);
       if (tiles < 0) continue;
       const int n = max(tiles, 1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
-      at += tiles + TokenPlaces::kEnd;
+      at += tiles + TokenPlaces<kRows>::kEnd;
       pos = min(at, st.hi);
       if (begin >= n) continue;                          // only the places of the item's end
       const int cut = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
       const int pages = rf_pages(it.len);
-      for (int t0 = begin; t0 < end; t0 += 32) {
+      const int stop = max(end, begin + C::GROUPS);      // every group gets a record, with nothing in it if there is no tile
+      for (int t0 = begin; t0 < stop; t0 += 32) {
         // a batch of tiles' entries, pages and scales: a lane each
         Record r;
         const int t = t0 + lane;
         int row = 0;
         r.item = item;
         r.page = t;
-        r.flags = cut | (t == begin ? kFirst : 0) | (t == end - 1 ? kLast : 0);
+        r.flags = cut | (t < begin + C::GROUPS ? kFirst : 0) | (t >= stop - C::GROUPS ? kLast : 0);
         r.k1 = r.k2 = r.v1 = r.v2 = 0u;
         if (t < end && t < tiles) {
           if (list != nullptr) r.page = list[t];
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
         } else {
           r.flags |= kNothing;
         }
-        const int batch = min(32, end - t0);
+        const int batch = min(32, stop - t0);
         for (int i = 0; i < batch; ++i) {
           Record s;
           s.item = item;
@@ -165,30 +173,32 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
           s.k2 = __shfl_sync(0xffffffffu, r.k2, i);
           s.v1 = __shfl_sync(0xffffffffu, r.v1, i);
           s.v2 = __shfl_sync(0xffffffffu, r.v2, i);
-          const int row_i = __shfl_sync(0xffffffffu, row, i);
-          if (lane == 0) publish(s, !(s.flags & kNothing), row_i);
+          const int row_i = __shfl_sync(0xffffffffu, row, i), group = (t0 + i - begin) % C::GROUPS;
+          if (lane == 0) publish(s, group, !(s.flags & kNothing), row_i);
           __syncwarp();
-          step();
+          if (group == 0) ++sent[0]; else ++sent[C::GROUPS - 1];
         }
       }
     }
-    if (lane == 0) publish(Record{0, 0, kEnd, 0, 0, 0, 0, 0}, false, 0);
+    if (lane == 0)
+      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0, 0, 0, 0, 0}, g, false, 0);
   } else {
-    // ------------------------------------------------------------ consumers: 16 keys of every tile each
-    const int g = lane >> 2, t = lane & 3;
-    uint32_t q[D / 16][4];
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, lx[2] = {0.f, 0.f};
-    int sees[2] = {0, 0};
+    // ------------------------------------------------------------ consumers: 16 keys of every tile of their group each
+    const int g = lane >> 2, t = lane & 3, group = warp >> 3, slice = 16 * (warp & 7);
+    uint32_t q[NB][D / 16][2];                 // B operands: row g of a block, four columns of every 16
+    float o[NB][D / 16][4], m[NB][2], l[NB][2], lx[NB][2];   // of rows 2t, 2t + 1 of a block
+    int sees[NB][2];
     uint32_t item_no = 0;
     CacheItem it = {};
     int stage = 0;
     uint32_t phase = 0;
     for (;;) {
+      const int slot = group * C::STAGES + stage;
       // (the warp as a whole: after an abandoned wait its lanes may differ in what they saw)
-      if (!__all_sync(0xffffffffu, mbar_wait_long(full(stage), phase, wc, 0))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait_long(full(slot), phase, wc, 0))) break;
       Record rec;
       {
-        volatile const Record* r = records + stage;
+        volatile const Record* r = records + slot;
         rec.item = r->item; rec.page = r->page; rec.flags = r->flags;
         rec.k1 = r->k1; rec.k2 = r->k2; rec.v1 = r->v1; rec.v2 = r->v2;
       }
@@ -197,84 +207,90 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
         it = cache_item<kRows>(a, rec.item);
         const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = it.r0 + g + 8 * i, place = r % a.u.M;
-          const bool there = r < a.u.rows && place < it.q_len;
-          sees[i] = there ? rf_row_sees(a.u.causal, it.len, it.q_len, place) : 0;
-          m[i] = -INFINITY;
-          l[i] = lx[i] = 0.f;
+        for (int nb = 0; nb < NB; ++nb) {
+          const int r = it.r0 + 8 * nb + g;
+          const bool there = r < a.u.rows && r % a.u.M < it.q_len;
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             uint2 x = make_uint2(0u, 0u);
             if (there) x = *reinterpret_cast<const uint2*>(src + (size_t)r * D + 16 * ks + 4 * t);
-            q[ks][i] = __byte_perm(x.x, x.y, 0x7632);          // columns 1 and 3 of the four, as widen_odd gives the keys'
-            q[ks][2 + i] = __byte_perm(x.x, x.y, 0x5410);      // columns 0 and 2
+            q[nb][ks][0] = __byte_perm(x.x, x.y, 0x7632);          // columns 1 and 3 of the four, as widen_odd gives the keys'
+            q[nb][ks][1] = __byte_perm(x.x, x.y, 0x5410);          // columns 0 and 2
           }
-        }
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+          for (int i = 0; i < 2; ++i) {
+            const int rs = it.r0 + 8 * nb + 2 * t + i, place = rs % a.u.M;
+            sees[nb][i] = rs < a.u.rows && place < it.q_len ? rf_row_sees(a.u.causal, it.len, it.q_len, place) : 0;
+            m[nb][i] = -INFINITY;
+            l[nb][i] = lx[nb][i] = 0.f;
+          }
+#pragma unroll
+          for (int n = 0; n < D / 16; ++n) o[nb][n][0] = o[nb][n][1] = o[nb][n][2] = o[nb][n][3] = 0.f;
+        }
       }
       if (!(rec.flags & kNothing)) {
-        const uint32_t kt = base + stage * 2 * C::TILE, vt = kt + C::TILE;
-        float s[2][4] = {};
+        const uint32_t kt = base + slot * 2 * C::TILE, vt = kt + C::TILE;
+        float s[NB][4] = {};                                       // keys g (0, 1) and g + 8 (2, 3) of the slice, rows 2t, 2t + 1
         const bool twice = rec.k2 != kOne2 || rec.v2 != kOne2;
         {
-          const int row = 16 * warp + (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
+          const int row = slice + (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
 #pragma unroll
           for (int ks = 0; ks < D / 16; ks += 2) {
             uint32_t x[4];
-            ldmatrix4(kt + C::chunk(row, ks + c0), x);
+            ldmatrix4(kt + C::chunk(row, ks + c0), x);              // keys 0-7: chunks ks, ks + 1; keys 8-15 likewise
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                       // keys 0-7: chunks ks, ks + 1; keys 8-15 likewise
-              uint32_t hi = mul_bf16x2(widen_odd(x[i]), rec.k1), lo = mul_bf16x2(widen_even(x[i]), rec.k1);
-              if (twice) { hi = mul_bf16x2(hi, rec.k2); lo = mul_bf16x2(lo, rec.k2); }
-              const int k = ks + (i & 1);
-              mma16816(s[i >> 1], q[k][0], q[k][1], q[k][2], q[k][3], hi, lo);
+            for (int i = 0; i < 2; ++i) {
+              uint32_t a0 = mul_bf16x2(widen_odd(x[i]), rec.k1), a2 = mul_bf16x2(widen_even(x[i]), rec.k1);
+              uint32_t a1 = mul_bf16x2(widen_odd(x[2 + i]), rec.k1), a3 = mul_bf16x2(widen_even(x[2 + i]), rec.k1);
+              if (twice) { a0 = mul_bf16x2(a0, rec.k2); a1 = mul_bf16x2(a1, rec.k2); a2 = mul_bf16x2(a2, rec.k2); a3 = mul_bf16x2(a3, rec.k2); }
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma16816(s[nb], a0, a1, a2, a3, q[nb][ks + i][0], q[nb][ks + i][1]);
             }
           }
         }
-        // scores to weights; key 8 nb + 2 t + e of this warp's sixteen, rows g and g + 8
-        const int key0 = rec.page * kPage + 16 * warp + 2 * t;
-        float alpha[2];
+        // scores to weights
+        const int key0 = rec.page * kPage + slice + g;
+        uint32_t p[NB][2];                                         // P^T as the second product's B operand
+        bool moved = false;
+        float alpha[NB][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float mx = -INFINITY;
+        for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-          for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float& x = s[nb][2 * i + e];
-              x = key0 + 8 * nb + e < sees[i] ? x * a.scale_log2 : -INFINITY;
-              mx = fmaxf(mx, x);
-            }
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float m_new = fmaxf(m[i], mx), use = m_new == -INFINITY ? 0.f : m_new;
-          alpha[i] = m_new == m[i] ? 1.f : ex2(m[i] - use);      // 0 from -inf on
-          m[i] = m_new;
-          float sum = 0.f, sumx = 0.f;
-#pragma unroll
-          for (int nb = 0; nb < 2; ++nb) {
-            const float p0 = ex2(s[nb][2 * i] - use), p1 = ex2(s[nb][2 * i + 1] - use);
-            const uint32_t pk = pack_bf16(p0, p1);               // P V multiplies the rounded weights: they normalise O
-            sum += __uint_as_float(pk << 16) + __uint_as_float(pk & 0xffff0000u);
-            if (LSE) sumx += p0 + p1;
-            s[nb][2 * i] = __uint_as_float(pk);
+          for (int i = 0; i < 2; ++i) {
+            float& x0 = s[nb][i];
+            float& x1 = s[nb][2 + i];
+            x0 = key0 < sees[nb][i] ? x0 * a.scale_log2 : -INFINITY;
+            x1 = key0 + 8 < sees[nb][i] ? x1 * a.scale_log2 : -INFINITY;
+            float mx = fmaxf(x0, x1);
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+            const float m_new = fmaxf(m[nb][i], mx), use = m_new == -INFINITY ? 0.f : m_new;
+            alpha[nb][i] = m_new == m[nb][i] ? 1.f : ex2(m[nb][i] - use);      // 0 from -inf on
+            moved |= m_new != m[nb][i];
+            m[nb][i] = m_new;
+            x0 = ex2(x0 - use);
+            x1 = ex2(x1 - use);
+            if (LSE) lx[nb][i] = lx[nb][i] * alpha[nb][i] + (x0 + x1);
           }
-          l[i] = l[i] * alpha[i] + sum;
-          if (LSE) lx[i] = lx[i] * alpha[i] + sumx;
+          const uint32_t p0 = pack_bf16(s[nb][0], s[nb][1]), p1 = pack_bf16(s[nb][2], s[nb][3]);   // P V multiplies the rounded weights: they normalise O
+          l[nb][0] = l[nb][0] * alpha[nb][0] + (__uint_as_float(p0 << 16) + __uint_as_float(p1 << 16));
+          l[nb][1] = l[nb][1] * alpha[nb][1] + (__uint_as_float(p0 & 0xffff0000u) + __uint_as_float(p1 & 0xffff0000u));
+          p[nb][0] = turn8x8(p0);
+          p[nb][1] = turn8x8(p1);
         }
-        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-          for (int n = 0; n < D / 8; ++n) { o[n][0] *= alpha[0]; o[n][1] *= alpha[0]; o[n][2] *= alpha[1]; o[n][3] *= alpha[1]; }
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) { o[nb][n][0] *= alpha[nb][0]; o[nb][n][1] *= alpha[nb][1]; o[nb][n][2] *= alpha[nb][0]; o[nb][n][3] *= alpha[nb][1]; }
         }
-        const uint32_t p0 = __float_as_uint(s[0][0]), p1 = __float_as_uint(s[0][2]), p2 = __float_as_uint(s[1][0]), p3 = __float_as_uint(s[1][2]);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
-          // word g + 8 j of keys 2t, 2t+1, 2t+8, 2t+9: columns 4 (g + 8 j) .. + 3
+          // word g + 8 j of keys 2t, 2t+1, 2t+8, 2t+9: columns 4 (g + 8 j) .. + 3, as rows g and g + 8 of two 16-row operands
           uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = lds32(vt + C::chunk(16 * warp + 2 * t + (i & 1) + 8 * (i >> 1), 2 * j + (g >> 2)) + (g & 3) * 4);
+          for (int i = 0; i < 4; ++i) w[i] = lds32(vt + C::chunk(slice + 2 * t + (i & 1) + 8 * (i >> 1), 2 * j + (g >> 2)) + (g & 3) * 4);
 #pragma unroll
           for (int hlf = 0; hlf < 2; ++hlf) {
             const uint32_t y = __byte_perm(w[0], w[1], hlf ? 0x7632 : 0x5410), z = __byte_perm(w[2], w[3], hlf ? 0x7632 : 0x5410);
@@ -284,48 +300,46 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
               ye = mul_bf16x2(ye, rec.v2); ze = mul_bf16x2(ze, rec.v2);
               yo = mul_bf16x2(yo, rec.v2); zo = mul_bf16x2(zo, rec.v2);
             }
-            mma16816(o[4 * j + 2 * hlf], p0, p1, p2, p3, ye, ze);
-            mma16816(o[4 * j + 2 * hlf + 1], p0, p1, p2, p3, yo, zo);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma16816(o[nb][2 * j + hlf], ye, yo, ze, zo, p[nb][0], p[nb][1]);
           }
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(empty(stage));
+      if (lane == 0) mbar_arrive(empty(slot));
       if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
       if (!(rec.flags & kLast)) continue;
 
-      // ---------------------------------------------------------- the item's (or piece's) end: the eight warps' rows meet
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int d = 1; d < 4; d <<= 1) {
-          l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
-          if (LSE) lx[i] += __shfl_xor_sync(0xffffffffu, lx[i], d);
-        }
-      }
+      // ---------------------------------------------------------- the item's (or piece's) end: the warps' rows meet
       const int n_rows = min(kRows, a.u.rows - it.r0);
       float* buf = reinterpret_cast<float*>(base_ptr + C::JOIN);
       float4* sums = reinterpret_cast<float4*>(base_ptr + C::SUMS);
       if (item_no > 0) mbar_wait(read, (item_no - 1) & 1, wc);    // the item before has been read
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = g + 8 * i;
-        if (r >= n_rows) continue;
-        if (t == 0) sums[warp * kRows + r] = make_float4(m[i], l[i], lx[i], 0.f);
-        float* row = buf + ((size_t)warp * kRows + r) * D;
+      for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j)
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            *reinterpret_cast<float4*>(row + 4 * (2 * t + e + 8 * j)) =
-                make_float4(o[4 * j][2 * i + e], o[4 * j + 1][2 * i + e], o[4 * j + 2][2 * i + e], o[4 * j + 3][2 * i + e]);
+          for (int d = 4; d < 32; d <<= 1) {
+            l[nb][i] += __shfl_xor_sync(0xffffffffu, l[nb][i], d);
+            if (LSE) lx[nb][i] += __shfl_xor_sync(0xffffffffu, lx[nb][i], d);
+          }
+          const int r = 8 * nb + 2 * t + i;
+          if (r >= n_rows) continue;
+          if (g == 0) sums[warp * kRows + r] = make_float4(m[nb][i], l[nb][i], lx[nb][i], 0.f);
+          float* row = buf + ((size_t)warp * kRows + r) * D;
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j)
+            *reinterpret_cast<float4*>(row + 4 * (g + 8 * j)) =
+                make_float4(o[nb][2 * j][i], o[nb][2 * j][2 + i], o[nb][2 * j + 1][i], o[nb][2 * j + 1][2 + i]);
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(joined);
       mbar_wait(joined, item_no & 1, wc);
       ++item_no;
       const bool piece = rec.flags & (kHeadPiece | kTailPiece);
-      float* slot = a.ws + head_floats(gridDim.x) + ((size_t)2 * blockIdx.x + (rec.flags & kTailPiece ? 1 : 0)) * C::PIECE;
+      float* out = a.ws + head_floats(gridDim.x) + ((size_t)2 * blockIdx.x + (rec.flags & kTailPiece ? 1 : 0)) * C::PIECE;
       for (int i = tid; i < n_rows * (D / 4); i += 32 * kWarps) {
         const int r = i / (D / 4), d4 = i % (D / 4), place = (it.r0 + r) % a.u.M;
         float mm = -INFINITY, ll = 0.f, llx = 0.f;
@@ -333,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
         for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sums[w * kRows + r].x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         const float use = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
+#pragma unroll 4
         for (int w = 0; w < kWarps; ++w) {
           const float4 sm = sums[w * kRows + r], x = *reinterpret_cast<const float4*>(buf + ((size_t)w * kRows + r) * D + d4 * 4);
           const float f = ex2(sm.x - use);
@@ -341,10 +355,10 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
           acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
         }
         if (piece) {
-          __stcg(reinterpret_cast<float4*>(slot + (size_t)r * D) + d4, acc);
-          if (d4 == 0) __stcg(reinterpret_cast<float4*>(slot + (size_t)kRows * D) + r, make_float4(mm, ll, llx, 0.f));
+          __stcg(reinterpret_cast<float4*>(out + (size_t)r * D) + d4, acc);
+          if (d4 == 0) __stcg(reinterpret_cast<float4*>(out + (size_t)kRows * D) + r, make_float4(mm, ll, llx, 0.f));
         } else if (place < it.q_len) {
-          const float inv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);   // (a sum that is no number stays one)
+          const float inv = ll == 0.f ? 0.f : 1.f / ll;            // (a sum that is no number stays one)
           const size_t at_row = (size_t)it.bh * a.u.rows + it.r0 + r;
           *reinterpret_cast<uint2*>(a.o + at_row * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
           if (LSE && d4 == 0) a.lse[at_row] = (mm + log2f(llx)) * 0.6931471805599453f;
@@ -360,9 +374,9 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_token_kernel(const __gri
 
 // Joins the pieces of the items that the stretches cut.  CTA x looks at the cut between stretches x and x + 1 and works if it is the
 // first one inside its item; blockIdx.y is the row.
-template <int D, bool LSE>
+template <int D, int NB, bool LSE>
 __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant__ RfCacheAttn a, int ctas) {
-  constexpr int PIECE = Cfg<D>::PIECE;
+  constexpr int kRows = 8 * NB, PIECE = Cfg<D, NB>::PIECE;
   __shared__ float red[2][D / 32];
   extern __shared__ float weight[];              // [ctas]
   rf_grid_trigger();
@@ -404,58 +418,61 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
     lx += sm.z * f;
     acc += __ldcg(at(i) + (size_t)r * D + tid) * f;
   }
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   const size_t at_row = (size_t)it.bh * a.u.rows + row;
   a.o[at_row * D + tid] = __float2bfloat16_rn(acc * inv);
   if (LSE && tid == 0) a.lse[at_row] = (mm + log2f(lx)) * 0.6931471805599453f;
 }
 
-// One CTA an SM; fewer where there is nothing to share out (a bound on the places of the line from the sizes alone).
-int token_ctas(const RfCache& c, const RfQueries& u) {
-  const long long items = (long long)c.B * c.H * rf_cdiv(u.rows, kRows), most = items * std::max(c.max_pages, 1);
-  return (int)std::min<long long>(most, 148);
-}
+constexpr int kMostRows = 16;
+int blocks_of(const RfQueries& u) { return u.rows <= 8 ? 1 : 2; }
 
-template <int D, bool LSE>
+// One CTA an SM; fewer where there is nothing to share out (a bound on the places of the line from the sizes alone).
+int token_ctas(const RfCache& c) { return (int)std::min<long long>((long long)c.B * c.H * (c.max_pages + 2ll), 148); }
+
+template <int D, int NB, bool LSE>
 rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
-  using C = Cfg<D>;
+  using C = Cfg<D, NB>;
   static bool configured[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return RF_ERR_CUDA;
   if (dev >= 0 && dev < 64 && !configured[dev]) {
-    if (cudaFuncSetAttribute(rf_cache_token_kernel<D, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::ALLOC) != cudaSuccess)
+    if (cudaFuncSetAttribute(rf_cache_token_kernel<D, NB, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::ALLOC) != cudaSuccess)
       return RF_ERR_CUDA;
     configured[dev] = true;
   }
   Maps maps;
   if (!rf_encode_pages_map(&maps.k, a.c.k, a.c) || !rf_encode_pages_map(&maps.v, a.c.v, a.c)) return RF_ERR_CUDA;
-  const int ctas = token_ctas(a.c, a.u);
-  if (rf_launch(rf_cache_token_kernel<D, LSE>, dim3(ctas), kThreads, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
+  const int ctas = token_ctas(a.c);
+  if (rf_launch(rf_cache_token_kernel<D, NB, LSE>, dim3(ctas), C::THREADS, C::ALLOC, st, maps, a) != cudaSuccess) return RF_ERR_CUDA;
   if (ctas == 1) return RF_OK;
-  const dim3 grid(ctas - 1, std::min(kRows, a.u.rows));
-  return rf_launch(rf_cache_join_kernel<D, LSE>, grid, D, sizeof(float) * (ctas + 1), st, a, ctas) == cudaSuccess ? RF_OK : RF_ERR_CUDA;
+  return rf_launch(rf_cache_join_kernel<D, NB, LSE>, dim3(ctas - 1, a.u.rows), D, sizeof(float) * (ctas + 1), st, a, ctas) == cudaSuccess ? RF_OK : RF_ERR_CUDA;
+}
+template <int D>
+rf_status launch(const RfCacheAttn& a, cudaStream_t st) {
+  if (blocks_of(a.u) == 1) return a.lse != nullptr ? launch<D, 1, true>(a, st) : launch<D, 1, false>(a, st);
+  return a.lse != nullptr ? launch<D, 2, true>(a, st) : launch<D, 2, false>(a, st);
 }
 
 }  // namespace
 
 namespace {
 // Whether a call's query rows are few: see the top of this file and of rf_cache_chunk.cu.
-bool few_rows(const RfQueries& u) { return u.rows <= kRows; }
+bool few_rows(const RfQueries& u) { return u.rows <= kMostRows; }
 }  // namespace
 
 size_t rf_cache_attn_ws_bytes(const RfCache& c, const RfQueries& u) {
   if (!few_rows(u)) return rf_cache_chunk_ws_bytes(c, u);
-  const int ctas = token_ctas(c, u);
-  return (head_floats(ctas) + (size_t)2 * ctas * kRows * (c.D + 4)) * sizeof(float);
+  const int ctas = token_ctas(c);
+  return (head_floats(ctas) + (size_t)2 * ctas * 8 * blocks_of(u) * (c.D + 4)) * sizeof(float);
 }
 
 rf_status rf_launch_cache_attn(const RfCacheAttn& a, cudaStream_t st) {
   if (!few_rows(a.u)) return rf_launch_cache_chunk(a, st);
-  const bool lse = a.lse != nullptr;
   switch (a.c.D) {
-    case 64: return lse ? launch<64, true>(a, st) : launch<64, false>(a, st);
-    case 96: return lse ? launch<96, true>(a, st) : launch<96, false>(a, st);
-    case 128: return lse ? launch<128, true>(a, st) : launch<128, false>(a, st);
+    case 64: return launch<64>(a, st);
+    case 96: return launch<96>(a, st);
+    case 128: return launch<128>(a, st);
   }
   return RF_ERR_UNSUPPORTED;
 }

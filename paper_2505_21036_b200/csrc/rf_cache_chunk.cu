@@ -103,7 +103,7 @@ struct Cfg {
 };
 
 // What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
-constexpr int kItemPlaces = 4;
+constexpr int kItemPlaces = 6;
 
 // The two streams' lists of an item: how long they are, how many keys their rows see at most.
 struct Streams { int n0, n1, sees0, sees1; };
