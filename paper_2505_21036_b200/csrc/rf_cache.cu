@@ -58,6 +58,7 @@ __host__ __device__ __forceinline__ PlanWs plan_ws(int32_t* ws, int B, int n_pag
 // Marks the pages that the table names; `lens` in shared memory, all in range; *most_pages (shared memory too) becomes the
 // longest row's number of pages.  False for everybody if an entry is none.
 __device__ __forceinline__ bool mark_pages(const RfCache& c, const int* lens, uint32_t* used, uint32_t* twice, int words, int* most_pages) {
+#pragma unroll 1
   for (int i = threadIdx.x; i < words; i += kPlanThreads) {
     used[i] = 0u;
     if (twice != nullptr) twice[i] = 0u;
@@ -70,6 +71,7 @@ __device__ __forceinline__ bool mark_pages(const RfCache& c, const int* lens, ui
   const int most = *most_pages;
   // Over the rows' used columns only.  (The products fit: n_seqs * max_pages < 2^33, in 64 bits.)
   const long long n = (long long)c.B * most;
+#pragma unroll 1
   for (long long i = threadIdx.x; i < n; i += kPlanThreads) {
     const int b = (int)(i / most), col = (int)(i - (long long)b * most);
     if (col >= rf_pages(lens[b])) continue;
@@ -126,6 +128,7 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
     return i == words - 1 && (c.n_pages & 31) ? f & ((1u << (c.n_pages & 31)) - 1u) : f;
   };
   int mine = 0;
+#pragma unroll 1
   for (int i = w0; i < w1; ++i) mine += __popc(free_of(i));
   int rank = block_scan(mine, scan, n_free);
   full = __syncthreads_or(full) || total > n_free;
@@ -136,7 +139,9 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
   }
   if (tid < c.B) need_at[tid] = at;
   if (tid == 0) need_at[c.B] = total;
+#pragma unroll 1
   for (int i = w0; i < w1 && rank < total; ++i)
+#pragma unroll 1
     for (uint32_t f = free_of(i); f != 0u && rank < total; f &= f - 1u) w.list[rank++] = i * 32 + __ffs(f) - 1;
   if (tid < c.B) {
     w.old_len[tid] = len;
@@ -146,8 +151,10 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
     lens[tid] = first_new - shared_page;       // the first column that gets a fresh page
   }
   __syncthreads();
+#pragma unroll 1
   for (int i = tid; i < total; i += kPlanThreads) {
     int lo = 0, hi = c.B - 1;                   // the last sequence whose pages begin at i or before
+#pragma unroll 1
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
       if (need_at[mid] <= i) lo = mid; else hi = mid - 1;
@@ -306,21 +313,26 @@ __global__ void __launch_bounds__(256) rf_cache_fork_kernel(RfCache c, const int
   rf_grid_trigger();
   rf_grid_wait();
   bool bad = false;
+#pragma unroll 1
   for (int b = tid; b < c.B; b += 256) bad |= parent[b] < -1 || parent[b] >= c.B;
+#pragma unroll 1
   for (int b = warp; b < c.B; b += 8)
     if (col < c.max_pages) rows[b * 32 + lane] = c.table[(size_t)b * c.max_pages + col];
   int* lens = rows + c.B * 32;
   if (blockIdx.x == 0)
+#pragma unroll 1
     for (int b = tid; b < c.B; b += 256) lens[b] = c.len[b];
   if (__syncthreads_or(bad)) {
     if (blockIdx.x == 0 && tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
     return;
   }
+#pragma unroll 1
   for (int b = warp; b < c.B; b += 8) {
     const int p = parent[b];
     if (p >= 0 && p != b && col < c.max_pages) c.table[(size_t)b * c.max_pages + col] = rows[p * 32 + lane];
   }
   if (blockIdx.x == 0)
+#pragma unroll 1
     for (int b = tid; b < c.B; b += 256) c.len[b] = parent[b] < 0 ? 0 : lens[parent[b]];
 }
 
@@ -329,6 +341,7 @@ __global__ void __launch_bounds__(256) rf_cache_drop_kernel(RfCache c, const int
   rf_grid_trigger();
   rf_grid_wait();
   bool bad = false;
+#pragma unroll 1
   for (int i = tid; i < c.B; i += 256) {
     if (max_len != nullptr) bad |= max_len[i] < 0;
     if (first != nullptr) bad |= first[i] < 0 || count[i] < 0;
@@ -348,6 +361,7 @@ __global__ void __launch_bounds__(256) rf_cache_drop_kernel(RfCache c, const int
     const int from = min(first[b], pages), n = min(count[b], pages - from);
     if (n > 0) {
       int32_t* row = c.table + (size_t)b * c.max_pages;
+#pragma unroll 1
       for (int base = from + n; base < pages; base += 256) {      // ascending: a stretch is read before it is written over
         const int i = base + tid, p = i < pages ? row[i] : 0;
         __syncthreads();
@@ -387,6 +401,7 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_compact_plan_kernel(RfC
   }
   const int per = (words + kPlanThreads - 1) / kPlanThreads, w0 = min(tid * per, words), w1 = min(w0 + per, words);
   int mine = 0, live, moves, n;
+#pragma unroll 1
   for (int i = w0; i < w1; ++i) mine += __popc(used[i]);
   block_scan(mine, scan, live);
   // bits of word i that lie before page `live`
@@ -395,14 +410,19 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_compact_plan_kernel(RfC
     return d >= 32 ? 0xffffffffu : d <= 0 ? 0u : (1u << d) - 1u;
   };
   int holes = 0, movers = 0;
+#pragma unroll 1
   for (int i = w0; i < w1; ++i) {
     holes += __popc(~used[i] & below(i));
     movers += __popc(used[i] & ~below(i));
   }
   int hole_at = block_scan(holes, scan, n), mover_at = block_scan(movers, scan, moves);   // n == moves
+#pragma unroll 1
   for (int i = w0; i < w1; ++i)
+#pragma unroll 1
     for (uint32_t f = ~used[i] & below(i); f != 0u; f &= f - 1u) w.to[hole_at++] = i * 32 + __ffs(f) - 1;
+#pragma unroll 1
   for (int i = w0; i < w1; ++i)
+#pragma unroll 1
     for (uint32_t f = used[i] & ~below(i); f != 0u; f &= f - 1u) w.list[mover_at++] = i * 32 + __ffs(f) - 1;
   if (tid == 0) {
     *w.count = moves;
@@ -410,6 +430,7 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_compact_plan_kernel(RfC
   }
   __syncthreads();
   const long long all = (long long)c.B * most;
+#pragma unroll 1
   for (long long i = tid; i < all; i += kPlanThreads) {
     const int b = (int)(i / most), col = (int)(i - (long long)b * most);
     if (col >= rf_pages(lens[b])) continue;
@@ -417,6 +438,7 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_compact_plan_kernel(RfC
     const int p = *entry;
     if (p < live) continue;
     int lo = 0, hi = moves - 1;                 // its place among the moving pages, which ascend
+#pragma unroll 1
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (w.list[mid] < p) lo = mid + 1; else hi = mid;
@@ -433,6 +455,7 @@ __global__ void __launch_bounds__(256) rf_cache_move_kernel(RfCache c, const int
   const PlanWs w = plan_ws(const_cast<int32_t*>(ws), c.B, c.n_pages);
   const int moves = *w.count, tid = threadIdx.x, n16 = kPage * c.D / 16;
   const long long items = (long long)moves * c.H * 2;
+#pragma unroll 1
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int m = (int)(it / (2 * c.H)), r = (int)(it % (2 * c.H)), h = r >> 1;
     const bool keys = (r & 1) == 0;
@@ -530,6 +553,7 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
       tail_sum[tid] = (float)sum * 0.001953125f * c.k_scale[side];
     }
     __syncthreads();
+#pragma unroll 1
     for (int i = tid; i < T * D; i += kSelThreads) {
       const int t = i / D, d = i % D;
       double x = 0.0;
@@ -538,6 +562,7 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
       pooled[d][t] = x;
     }
     __syncthreads();
+#pragma unroll 1
     for (int c0 = keep_first + warp * 32; c0 < most; c0 += kSelThreads) {
       const int col = c0 + lane;
       const bool there = col < most;
@@ -570,9 +595,12 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
     // the best-th largest: eight bits at a time
     uint64_t prefix = 0ull;
     int need = best;
+#pragma unroll 1
     for (int shift = 56; shift >= 0; shift -= 8) {
+#pragma unroll 1
       for (int i = rank; i < 256; i += kTeam) hist[mine][i] = 0;
       team_sync();
+#pragma unroll 1
       for (int base = first_end + wrank * 32; base < last_begin; base += kTeam) {
         const int i = base + lane;
         const uint64_t k = i < last_begin ? key[i] : 0ull;
@@ -628,6 +656,7 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
   }
   // the list, in order
   int out = 0, ties = 0;
+#pragma unroll 1
   for (int base = 0; base < n; base += kTeam) {
     const int col = base + rank;
     const bool always = col < n && (col < first_end || col >= last_begin);

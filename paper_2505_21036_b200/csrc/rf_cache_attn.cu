@@ -4,7 +4,11 @@
 // the cache's bytes at the HBM rate: an SM has 1400 cycles for the 32 KB of a tile of 128 keys at D = 128.
 // A producer warp streams the tiles into rings in shared memory by TMA (page by page, swizzled, 128 KB under way).  Eight warps
 // take 16 keys of a tile each, on mma.sync with the keys as its 16 rows and the queries as its 8 columns (tcgen05 would spend 128 rows on
-// them): S^T = K q^T, then O^T += V^T P^T with P^T turned round by movmatrix.  Codes are widened to bf16 in registers, exactly.  The order
+// them): S^T = K q^T, then O^T += V^T P^T with P^T turned round by movmatrix.  Codes are widened to fp16 in registers, exactly, by one
+// conversion a pair (to bf16 it takes seven integer instructions and two products for four, and the integer pipe was what bound it: 152 us
+// for 33 frames of 3600 tokens, 24 heads).  So the other operands are fp16 too: a query row scaled by a power of two to a largest
+// magnitude in [2^14, 2^15) (exact down to 2^-29 of that, 2^-40 of it beyond), and the weights times 2^15, whose largest is exact here
+// (11 bits, to 2^-39 of the largest).  The scales of rows and pages are applied in fp32.  The order
 // of a contraction is free, so the words are used as they lie: a word of K is four of the 16 terms of one instruction, and V's bytes
 // of two keys are brought together by one byte permutation.  Up to 8 rows, two groups of eight warps take the tiles in turn, four warps
 // to a scheduler (one group, and queries as rows of the product: 190 us for 33 frames of 3600 tokens, 24 heads, where the bytes take 112);
@@ -42,7 +46,7 @@ struct Cfg {
   }
 };
 
-struct Record { int item, page, flags; uint32_t k1, k2, v1, v2; int pad; };
+struct Record { int item, page, flags; float ks, vs; };
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -53,9 +57,26 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
   return v;
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// Bytes 0 and 1, bytes 2 and 3 of a word of codes as fp16 pairs.
+__device__ __forceinline__ uint32_t widen_low(uint32_t x) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(d) : "r"(x));
+  return d;
+}
+__device__ __forceinline__ uint32_t widen_high(uint32_t x) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(d) : "r"(x));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 t = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+constexpr float kWeightUnit = 32768.f;           // the weights' largest
+
 __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   uint32_t d;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
@@ -70,7 +91,7 @@ __device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem&
 template <int kRows>
 struct TokenPlaces {
   static constexpr int kRowsOf = kRows, kEnd = 2;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
-  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+  static __device__ __noinline__ int of(const RfCacheAttn& a, int item) {
     const int n = item_tiles(a, cache_item<kRows>(a, item));
     return n < 0 ? 0 : n + kEnd;
   }
@@ -93,6 +114,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
   StretchScratch* scratch = reinterpret_cast<StretchScratch*>(base_ptr + C::MISC + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
+#pragma unroll 1
     for (int s = 0; s < C::SLOTS; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 8); }
     mbar_init(joined, kWarps);
     mbar_init(read, kWarps);
@@ -116,10 +138,10 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     long long at = st.at;
     auto publish = [&](const Record& r, int group, bool bytes, int row) {   // lane 0
       const int n = sent[group], s = group * C::STAGES + n % C::STAGES;
-      if (!mbar_wait(empty(s), ((n / C::STAGES) & 1) ^ 1, wc)) return;        // (the first round finds them free) abandoned: nothing more is fetched
+      if (!wait_for(empty(s), ((n / C::STAGES) & 1) ^ 1, wc)) return;        // (the first round finds them free) abandoned: nothing more is fetched
       volatile Record* d = records + s;
       d->item = r.item; d->page = r.page; d->flags = r.flags;
-      d->k1 = r.k1; d->k2 = r.k2; d->v1 = r.v1; d->v2 = r.v2;
+      d->ks = r.ks; d->vs = r.vs;
       if (bytes) {
         const uint32_t to = base + s * 2 * C::TILE;
         mbar_expect_tx(full(s), 2 * C::TILE);
@@ -129,6 +151,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
         mbar_arrive(full(s));
       }
     };
+#pragma unroll 1
     for (long long pos = st.lo; pos < st.hi; ++item) {
       const CacheItem it = cache_item<kRows>(a, item);
       const int tiles = item_tiles(a, it);
@@ -141,6 +164,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
       const int pages = rf_pages(it.len);
       const int stop = max(end, begin + C::GROUPS);      // every group gets a record, with nothing in it if there is no tile
+#pragma unroll 1
       for (int t0 = begin; t0 < stop; t0 += 32) {
         // a batch of tiles' entries, pages and scales: a lane each
         Record r;
@@ -149,7 +173,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
         r.item = item;
         r.page = t;
         r.flags = cut | (t < begin + C::GROUPS ? kFirst : 0) | (t >= stop - C::GROUPS ? kLast : 0);
-        r.k1 = r.k2 = r.v1 = r.v2 = 0u;
+        r.ks = r.vs = 0.f;
         if (t < end && t < tiles) {
           if (list != nullptr) r.page = list[t];
           if (r.page < 0 || r.page >= pages) {
@@ -157,22 +181,21 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
             r.flags |= kNothing;
           } else {
             row = rf_page(a.c, it.b, r.page, a.dev_status) * a.c.H + it.bh % a.c.H;
-            const Widen k = widen_by(a.c.k_scale[row]), v = widen_by(a.c.v_scale[row]);
-            r.k1 = k.m1; r.k2 = k.m2; r.v1 = v.m1; r.v2 = v.m2;
+            r.ks = a.c.k_scale[row];
+            r.vs = a.c.v_scale[row];
           }
         } else {
           r.flags |= kNothing;
         }
         const int batch = min(32, stop - t0);
+#pragma unroll 1
         for (int i = 0; i < batch; ++i) {
           Record s;
           s.item = item;
           s.page = __shfl_sync(0xffffffffu, r.page, i);
           s.flags = __shfl_sync(0xffffffffu, r.flags, i);
-          s.k1 = __shfl_sync(0xffffffffu, r.k1, i);
-          s.k2 = __shfl_sync(0xffffffffu, r.k2, i);
-          s.v1 = __shfl_sync(0xffffffffu, r.v1, i);
-          s.v2 = __shfl_sync(0xffffffffu, r.v2, i);
+          s.ks = __shfl_sync(0xffffffffu, r.ks, i);
+          s.vs = __shfl_sync(0xffffffffu, r.vs, i);
           const int row_i = __shfl_sync(0xffffffffu, row, i), group = (t0 + i - begin) % C::GROUPS;
           if (lane == 0) publish(s, group, !(s.flags & kNothing), row_i);
           __syncwarp();
@@ -181,46 +204,68 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       }
     }
     if (lane == 0)
-      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0, 0, 0, 0, 0}, g, false, 0);
+#pragma unroll 1
+      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0.f, 0.f}, g, false, 0);
   } else {
     // ------------------------------------------------------------ consumers: 16 keys of every tile of their group each
     const int g = lane >> 2, t = lane & 3, group = warp >> 3, slice = 16 * (warp & 7);
     uint32_t q[NB][D / 16][2];                 // B operands: row g of a block, four columns of every 16
     float o[NB][D / 16][4], m[NB][2], l[NB][2], lx[NB][2];   // of rows 2t, 2t + 1 of a block
     int sees[NB][2];
+    float rs[NB][2];                           // those rows' factor of the scores
     uint32_t item_no = 0;
     CacheItem it = {};
     int stage = 0;
     uint32_t phase = 0;
+#pragma unroll 1
     for (;;) {
       const int slot = group * C::STAGES + stage;
       // (the warp as a whole: after an abandoned wait its lanes may differ in what they saw)
-      if (!__all_sync(0xffffffffu, mbar_wait_long(full(slot), phase, wc, 0))) break;
+      if (!__all_sync(0xffffffffu, wait_for(full(slot), phase, wc))) break;
       Record rec;
       {
         volatile const Record* r = records + slot;
         rec.item = r->item; rec.page = r->page; rec.flags = r->flags;
-        rec.k1 = r->k1; rec.k2 = r->k2; rec.v1 = r->v1; rec.v2 = r->v2;
+        rec.ks = r->ks; rec.vs = r->vs;
       }
       if (rec.flags & kEnd) break;
       if (rec.flags & kFirst) {
         it = cache_item<kRows>(a, rec.item);
         const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
+        int row_sees = -1;                                         // keys that row `lane` sees; -1: it is not there
+        if (lane < kRows && it.r0 + lane < a.u.rows) {
+          const int place = (it.r0 + lane) % a.u.M;
+          if (place < it.q_len) row_sees = rf_row_sees(a.u.causal, it.len, it.q_len, place);
+        }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const int r = it.r0 + 8 * nb + g;
-          const bool there = r < a.u.rows && r % a.u.M < it.q_len;
+          const bool there = __shfl_sync(0xffffffffu, row_sees, 8 * nb + g) >= 0;
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             uint2 x = make_uint2(0u, 0u);
             if (there) x = *reinterpret_cast<const uint2*>(src + (size_t)r * D + 16 * ks + 4 * t);
-            q[nb][ks][0] = __byte_perm(x.x, x.y, 0x7632);          // columns 1 and 3 of the four, as widen_odd gives the keys'
-            q[nb][ks][1] = __byte_perm(x.x, x.y, 0x5410);          // columns 0 and 2
+            q[nb][ks][0] = x.x;                                    // columns 0 and 1 of the four, as widen_low gives the keys'
+            q[nb][ks][1] = x.y;
           }
+          uint32_t most = 0u;                                      // the row's largest magnitude, as bf16 bits
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) most = max(most, max(q[nb][ks][i] & 0x7fffu, (q[nb][ks][i] >> 16) & 0x7fffu));
+          most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+          most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+          const int e = most == 0u ? 0 : min(14 - ((int)(most >> 7) - 127), 126);
+          const float up = __uint_as_float((uint32_t)(e + 127) << 23), down = a.scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              q[nb][ks][i] = pack_f16(__uint_as_float(q[nb][ks][i] << 16) * up, __uint_as_float(q[nb][ks][i] & 0xffff0000u) * up);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int rs = it.r0 + 8 * nb + 2 * t + i, place = rs % a.u.M;
-            sees[nb][i] = rs < a.u.rows && place < it.q_len ? rf_row_sees(a.u.causal, it.len, it.q_len, place) : 0;
+            sees[nb][i] = max(__shfl_sync(0xffffffffu, row_sees, 8 * nb + 2 * t + i), 0);
+            rs[nb][i] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + i));
             m[nb][i] = -INFINITY;
             l[nb][i] = lx[nb][i] = 0.f;
           }
@@ -231,7 +276,6 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       if (!(rec.flags & kNothing)) {
         const uint32_t kt = base + slot * 2 * C::TILE, vt = kt + C::TILE;
         float s[NB][4] = {};                                       // keys g (0, 1) and g + 8 (2, 3) of the slice, rows 2t, 2t + 1
-        const bool twice = rec.k2 != kOne2 || rec.v2 != kOne2;
         {
           const int row = slice + (lane & 7) + ((lane >> 4) << 3), c0 = (lane >> 3) & 1;
 #pragma unroll
@@ -240,9 +284,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
             ldmatrix4(kt + C::chunk(row, ks + c0), x);              // keys 0-7: chunks ks, ks + 1; keys 8-15 likewise
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              uint32_t a0 = mul_bf16x2(widen_odd(x[i]), rec.k1), a2 = mul_bf16x2(widen_even(x[i]), rec.k1);
-              uint32_t a1 = mul_bf16x2(widen_odd(x[2 + i]), rec.k1), a3 = mul_bf16x2(widen_even(x[2 + i]), rec.k1);
-              if (twice) { a0 = mul_bf16x2(a0, rec.k2); a1 = mul_bf16x2(a1, rec.k2); a2 = mul_bf16x2(a2, rec.k2); a3 = mul_bf16x2(a3, rec.k2); }
+              const uint32_t a0 = widen_low(x[i]), a1 = widen_low(x[2 + i]), a2 = widen_high(x[i]), a3 = widen_high(x[2 + i]);
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb) mma16816(s[nb], a0, a1, a2, a3, q[nb][ks + i][0], q[nb][ks + i][1]);
             }
@@ -259,8 +301,8 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
           for (int i = 0; i < 2; ++i) {
             float& x0 = s[nb][i];
             float& x1 = s[nb][2 + i];
-            x0 = key0 < sees[nb][i] ? x0 * a.scale_log2 : -INFINITY;
-            x1 = key0 + 8 < sees[nb][i] ? x1 * a.scale_log2 : -INFINITY;
+            x0 = key0 < sees[nb][i] ? x0 * (rs[nb][i] * rec.ks) : -INFINITY;
+            x1 = key0 + 8 < sees[nb][i] ? x1 * (rs[nb][i] * rec.ks) : -INFINITY;
             float mx = fmaxf(x0, x1);
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
@@ -269,13 +311,14 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
             alpha[nb][i] = m_new == m[nb][i] ? 1.f : ex2(m[nb][i] - use);      // 0 from -inf on
             moved |= m_new != m[nb][i];
             m[nb][i] = m_new;
-            x0 = ex2(x0 - use);
-            x1 = ex2(x1 - use);
-            if (LSE) lx[nb][i] = lx[nb][i] * alpha[nb][i] + (x0 + x1);
+            x0 = ex2(x0 - use + 15.f);                             // in units of 2^-15
+            x1 = ex2(x1 - use + 15.f);
+            if (LSE) lx[nb][i] = lx[nb][i] * alpha[nb][i] + (x0 + x1) * (1.f / kWeightUnit);
           }
-          const uint32_t p0 = pack_bf16(s[nb][0], s[nb][1]), p1 = pack_bf16(s[nb][2], s[nb][3]);   // P V multiplies the rounded weights: they normalise O
-          l[nb][0] = l[nb][0] * alpha[nb][0] + (__uint_as_float(p0 << 16) + __uint_as_float(p1 << 16));
-          l[nb][1] = l[nb][1] * alpha[nb][1] + (__uint_as_float(p0 & 0xffff0000u) + __uint_as_float(p1 & 0xffff0000u));
+          const uint32_t p0 = pack_f16(s[nb][0], s[nb][1]), p1 = pack_f16(s[nb][2], s[nb][3]);   // P V multiplies the rounded weights: they normalise O
+          const float2 w0 = __half22float2(*reinterpret_cast<const __half2*>(&p0)), w1 = __half22float2(*reinterpret_cast<const __half2*>(&p1));
+          l[nb][0] = l[nb][0] * alpha[nb][0] + (w0.x + w1.x) * (1.f / kWeightUnit);
+          l[nb][1] = l[nb][1] * alpha[nb][1] + (w0.y + w1.y) * (1.f / kWeightUnit);
           p[nb][0] = turn8x8(p0);
           p[nb][1] = turn8x8(p1);
         }
@@ -285,23 +328,30 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
 #pragma unroll
             for (int n = 0; n < D / 16; ++n) { o[nb][n][0] *= alpha[nb][0]; o[nb][n][1] *= alpha[nb][1]; o[nb][n][2] *= alpha[nb][0]; o[nb][n][3] *= alpha[nb][1]; }
         }
+        const float vs = rec.vs * (1.f / kWeightUnit);
+        const int valid = it.len - rec.page * kPage - slice;       // of this warp's keys; what lies behind them may be no numbers
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
           // word g + 8 j of keys 2t, 2t+1, 2t+8, 2t+9: columns 4 (g + 8 j) .. + 3, as rows g and g + 8 of two 16-row operands
           uint32_t w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = lds32(vt + C::chunk(slice + 2 * t + (i & 1) + 8 * (i >> 1), 2 * j + (g >> 2)) + (g & 3) * 4);
+          if (valid < 16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (2 * t + (i & 1) + 8 * (i >> 1) >= valid) w[i] = 0u;
+          }
 #pragma unroll
           for (int hlf = 0; hlf < 2; ++hlf) {
-            const uint32_t y = __byte_perm(w[0], w[1], hlf ? 0x7632 : 0x5410), z = __byte_perm(w[2], w[3], hlf ? 0x7632 : 0x5410);
-            uint32_t ye = mul_bf16x2(widen_even(y), rec.v1), ze = mul_bf16x2(widen_even(z), rec.v1);
-            uint32_t yo = mul_bf16x2(widen_odd(y), rec.v1), zo = mul_bf16x2(widen_odd(z), rec.v1);
-            if (twice) {
-              ye = mul_bf16x2(ye, rec.v2); ze = mul_bf16x2(ze, rec.v2);
-              yo = mul_bf16x2(yo, rec.v2); zo = mul_bf16x2(zo, rec.v2);
-            }
+            const uint32_t y = __byte_perm(w[0], w[1], hlf ? 0x7362 : 0x5140), z = __byte_perm(w[2], w[3], hlf ? 0x7362 : 0x5140);
+            const uint32_t a0 = widen_low(y), a1 = widen_high(y), a2 = widen_low(z), a3 = widen_high(z);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma16816(o[nb][2 * j + hlf], ye, yo, ze, zo, p[nb][0], p[nb][1]);
+            for (int nb = 0; nb < NB; ++nb) {
+              float tile[4] = {};
+              mma16816(tile, a0, a1, a2, a3, p[nb][0], p[nb][1]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[nb][2 * j + hlf][i] += tile[i] * vs;
+            }
           }
         }
       }
@@ -314,7 +364,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       const int n_rows = min(kRows, a.u.rows - it.r0);
       float* buf = reinterpret_cast<float*>(base_ptr + C::JOIN);
       float4* sums = reinterpret_cast<float4*>(base_ptr + C::SUMS);
-      if (item_no > 0) mbar_wait(read, (item_no - 1) & 1, wc);    // the item before has been read
+      if (item_no > 0) wait_for(read, (item_no - 1) & 1, wc);    // the item before has been read
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
@@ -336,14 +386,15 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(joined);
-      mbar_wait(joined, item_no & 1, wc);
+      wait_for(joined, item_no & 1, wc);
       ++item_no;
       const bool piece = rec.flags & (kHeadPiece | kTailPiece);
       float* out = a.ws + head_floats(gridDim.x) + ((size_t)2 * blockIdx.x + (rec.flags & kTailPiece ? 1 : 0)) * C::PIECE;
+#pragma unroll 1
       for (int i = tid; i < n_rows * (D / 4); i += 32 * kWarps) {
         const int r = i / (D / 4), d4 = i % (D / 4), place = (it.r0 + r) % a.u.M;
         float mm = -INFINITY, ll = 0.f, llx = 0.f;
-#pragma unroll
+#pragma unroll 4
         for (int w = 0; w < kWarps; ++w) mm = fmaxf(mm, sums[w * kRows + r].x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         const float use = mm == -INFINITY ? 0.f : mm;
@@ -389,6 +440,7 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
   const int32_t* prev = mine - kHeadWords;
   if (prev[3] && prev[0] == mine[0]) return;
   int n = 1;                                     // stretches x .. x + n - 1 begin inside the item
+#pragma unroll 1
   while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
   const CacheItem it = cache_item<kRows>(a, mine[0]);
   const int row = it.r0 + r;
@@ -397,6 +449,7 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
   // piece 0 is the one that stretch x - 1 ends in, piece i > 0 the one that stretch x + i - 1 begins in
   auto at = [&](int i) -> const float* { return pieces + (i == 0 ? (size_t)2 * (x - 1) + 1 : (size_t)2 * (x + i - 1)) * PIECE; };
   float mm = -INFINITY;
+#pragma unroll 1
   for (int i = tid; i <= n; i += D) {
     const float m = __ldcg(at(i) + (size_t)kRows * D + r * 4);
     weight[i] = m;

@@ -17,10 +17,20 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// A bounded wait (see mbar_wait_long) whose slow part is called, not inlined.  A kernel here starts with cold instruction caches, as a
+// layer runs other kernels in between, and fetches its code from the L2 line by line: what is not straight on the way is kept short or
+// out of line.
+static __device__ __noinline__ bool wait_slowly(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* dev_status, int tiles) {
+  return sm100::mbar_wait_long(bar, parity, sm100::WaitCtx{abort_flag, dev_status}, tiles);
+}
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const sm100::WaitCtx& w, int tiles = 0) {
+  return sm100::mbar_try(bar, parity) || wait_slowly(bar, parity, w.abort_flag, w.dev_status, tiles);
+}
+
 // An item: rows [r0, r0 + kRows) of K/V head bh.
 struct CacheItem { int b, bh, r0, len, q_len, sees; };
 template <int kRows>
-__device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
+static __device__ __noinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
   const int blocks = rf_cdiv(a.u.rows, kRows);
   CacheItem it;
   it.bh = item / blocks;
@@ -49,6 +59,7 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
   const int items = a.c.B * a.c.H * rf_cdiv(a.u.rows, Places::kRowsOf), per = rf_cdiv(items, kThreads);
   const int i0 = min(tid * per, items), i1 = min(i0 + per, items);
   long long mine = 0;
+#pragma unroll 1
   for (int i = i0; i < i1; ++i) mine += Places::of(a, i);
   long long x = mine;
 #pragma unroll
@@ -59,6 +70,7 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
   if (lane == 31) s->sums[warp] = x;
   __syncthreads();
   long long before = x - mine, total = 0;
+#pragma unroll 1
   for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) before += s->sums[w];
     total += s->sums[w];
@@ -70,6 +82,7 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
   if (lo < hi && before <= lo && lo < before + mine) {
     long long at = before;
     int i = i0;
+#pragma unroll 1
     for (;; ++i) {
       const int p = Places::of(a, i);
       if (lo < at + p) {

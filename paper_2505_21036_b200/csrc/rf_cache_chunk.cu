@@ -107,7 +107,7 @@ constexpr int kItemPlaces = 6;
 
 // The two streams' lists of an item: how long they are, how many keys their rows see at most.
 struct Streams { int n0, n1, sees0, sees1; };
-__device__ __forceinline__ Streams streams(const RfCacheAttn& a, const CacheItem& it) {
+static __device__ __noinline__ Streams streams(const RfCacheAttn& a, const CacheItem& it) {
   Streams s;
   const int tile = it.r0 / kPage;
   s.sees0 = rf_rows_see(a.u, it.len, it.q_len, it.r0, BM);
@@ -123,7 +123,7 @@ __device__ __forceinline__ Streams streams(const RfCacheAttn& a, const CacheItem
 }
 struct ChunkPlaces {
   static constexpr int kRowsOf = kRows, kEnd = kItemPlaces;
-  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+  static __device__ __noinline__ int of(const RfCacheAttn& a, int item) {
     const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
     if (it.sees < 0) return 0;
     const Streams s = streams(a, it);
@@ -180,7 +180,9 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     mbar_init(bar(C::B_Q), 4);
     mbar_init(bar(C::B_QE), 1);
     mbar_init(bar(C::B_QR), 1);
+#pragma unroll 1
     for (int s = 0; s < C::NK; ++s) { mbar_init(bar(C::B_KF + s), 1); mbar_init(bar(C::B_KE + s), 1); }
+#pragma unroll 1
     for (int s = 0; s < C::NV; ++s) { mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1); }
     for (int j = 0; j < 2; ++j) {
       mbar_init(bar(C::B_SF + j), 1);
@@ -188,11 +190,14 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       mbar_init(bar(C::B_OF + j), 1);
       mbar_init(bar(C::B_SE + j), 4);
     }
+#pragma unroll 1
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(bar(C::B_IF + i), 1); mbar_init(bar(C::B_IE + i), kItemReaders); }
+#pragma unroll 1
     for (int i = 0; i < C::NS; ++i) { mbar_init(bar(C::B_CF + i), 1); mbar_init(bar(C::B_CE + i), 4); }
     *abort_flag = 0;
     mbar_init_fence();
   }
+#pragma unroll 1
   for (int i = tid; i < C::NV * BN * 2; i += kThreads) {   // the 16 columns behind V's: one, then zeros
     const int v = i / (BN * 2), row = i / 2 % BN, c = i % 2;
     *reinterpret_cast<uint4*>(base_ptr + C::V0 + v * C::VTILE + C::VLOAD + C::vchunk(row, c)) = make_uint4(c == 0 ? 0x3f80u : 0u, 0u, 0u, 0u);
@@ -269,14 +274,15 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       }
     };
     int nq = 0;                               // items with tiles so far
+#pragma unroll 1
     for (int u = 0;; ++u) {
       const int cs = u % C::NS, vs = u % C::NV;
-      if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_CF + cs), (u / C::NS) & 1, wc, 0))) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(C::B_CF + cs), (u / C::NS) & 1, wc))) break;
       volatile const uint32_t* r = records + cs * 4;
       const uint32_t f = r[0], m1 = r[1], m2 = r[2];
       if (!(f & kMore)) break;
       if (f & kFirst) {
-        if (!__all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QR), nq & 1, wc, 0))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(C::B_QR), nq & 1, wc))) break;
         ++nq;
         split_q((int)r[3]);
         fence_proxy_async_smem();
@@ -319,6 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       long long at = st.at;
       int item = st.item;
       bool ok = true;
+#pragma unroll 1
       for (long long pos = st.lo; pos < st.hi && ok; ++item) {
         const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
         if (it.sees < 0) continue;
@@ -350,6 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
         const int32_t* l1 = l0 != nullptr && it.r0 / kPage + 1 < a.u.n_q ? l0 + a.n_k : l0;
         int i0 = b0, i1 = b1;
+#pragma unroll 1
         while ((i0 < e0 || i1 < e1) && ok) {
           // a batch of the union: entries past the sequence count as page `pages`, which no row sees
           int m0 = 0x7fffffff, m1 = 0x7fffffff;
@@ -364,6 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           __syncwarp();
           int take0 = 0, take1 = 0, cnt = 0;
           if (lane == 0) {
+#pragma unroll 1
             for (; cnt < kBatch; ++cnt) {
               const int h0 = take0 < kBatch ? win[take0] : 0x7fffffff, h1 = take1 < kBatch ? win[kBatch + take1] : 0x7fffffff;
               const int h = min(h0, h1);
@@ -392,16 +401,17 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             vw = rf_cache_attn::widen_by(a.c.v_scale[row]);
           }
           // the tiles one after the other, each by the lane that looked it up
+#pragma unroll 1
           for (int i = 0; i < cnt && ok; ++i, ++u) {
             const int cs = u % C::NS, ks = u % C::NK;
-            if (u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0));
+            if (u >= C::NK) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc));
             if (ok && lane == i) {
               flags[ks] = f;
               mbar_expect_tx(bar(C::B_KF + ks), C::TILE);
               tma_load_3d(base + C::K0 + ks * C::TILE, &maps.k, 0, 0, (int)row, bar(C::B_KF + ks));
             }
             if (ok && first) {                                     // the item before has taken its last scores: its Q may go
-              if (nq > 0) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_QE), (nq - 1) & 1, wc, 0));
+              if (nq > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_QE), (nq - 1) & 1, wc));
               if (ok && lane == 0) {
                 constexpr uint32_t kBlock = 128 * 128;             // 128 rows of 64 bf16
                 mbar_expect_tx(bar(C::B_QR), 2 * ((D + 63) / 64) * kBlock);
@@ -414,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
               ++nq;
               first = false;
             }
-            if (ok && u >= C::NS) ok = __all_sync(0xffffffffu, mbar_wait_long(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc, 0));
+            if (ok && u >= C::NS) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc));
             if (ok && lane == i) {
               volatile uint32_t* r = records + cs * 4;
               r[0] = f; r[1] = vw.m1; r[2] = vw.m2; r[3] = slot;
@@ -427,8 +437,8 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       }
       // the end, for the warps that walk tiles and for those that walk items
       const int cs = u % C::NS, slot = no % kItemSlots, ks = u % C::NK;
-      if (u >= C::NK) mbar_wait_long(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc, 0);
-      if (u >= C::NS) mbar_wait_long(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc, 0);
+      if (u >= C::NK) mbar_wait(bar(C::B_KE + ks), ((u / C::NK) - 1) & 1, wc);
+      if (u >= C::NS) mbar_wait(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc);
       if (no >= kItemSlots) mbar_wait_long(bar(C::B_IE + slot), ((no / kItemSlots) - 1) & 1, wc, (int)min(st.hi - st.lo, 1ll << 20));
       if (lane == 0) {
         records[cs * 4] = 0;
@@ -484,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         };
         // the next tile's flags, once its K is in place; nothing after an abandoned wait
         auto next = [&](int u) -> uint32_t {
-          if (!mbar_wait_long(bar(C::B_KF + u % C::NK), (u / C::NK) & 1, wc, 0)) return 0u;
+          if (!mbar_wait(bar(C::B_KF + u % C::NK), (u / C::NK) & 1, wc)) return 0u;
           tc_fence_after();
           return flags[u % C::NK];
         };
@@ -501,6 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         };
         cur = next(0);
         if (cur & kMore) open(cur, 0);
+#pragma unroll 1
         for (int u = 0; cur & kMore; ++u) {
           const int vs = u % C::NV, ks = (u + 1) % C::NK;
           uint32_t nxt = 0;
@@ -562,6 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     const float sc = a.scale_log2;
     uint32_t done = 0, nq = 0;
     int waited = 0;
+#pragma unroll 1
     for (int item = 0;; ++item) {
       const int slot = item % kItemSlots;
       const int* iw = items + slot * kItemWords;
@@ -596,6 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         row_scale *= __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
       }
       bool opens = true;
+#pragma unroll 1
       for (int t = begin; t < end; ++t, ++done, opens = false) {
         const int left = sees - page_next * kPage;        // keys of the tile that this row sees (page <= 2^23: no overflow)
         float sc = row_scale * ks_next;
@@ -797,6 +810,7 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   if (!mine[3]) return;
   if (mine[3 - kHeadWords] && mine[-kHeadWords] == mine[0]) return;
   int n = 1;
+#pragma unroll 1
   while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
   const CacheItem it = rf_cache_attn::cache_item<kRows>(a, mine[0]);
   const int row = it.r0 + j * BM + threadIdx.x;
@@ -804,6 +818,7 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   const float4* pieces = reinterpret_cast<const float4*>(a.ws + head_floats(ctas)) + threadIdx.x;
   float m = -INFINITY, l = 0.f, lx = 0.f;
   float4 acc[4] = {};
+#pragma unroll 1
   for (int i = 0; i <= n; ++i) {
     const float4* at = pieces + ((i == 0 ? (size_t)2 * (x - 1) + 1 : (size_t)2 * (x + i - 1)) * 2 + j) * C::PIECE;
     const float4 st = __ldcg(at + (D / 4) * BM);
