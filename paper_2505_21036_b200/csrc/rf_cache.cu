@@ -508,7 +508,6 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int mine = warp / kOf, rank = tid % kTeam, wrank = warp % kOf;     // this thread's tile, and its place in the tile's team
   const int tile = blockIdx.x * T + mine, h = blockIdx.y, b = blockIdx.z;
-  rf_grid_trigger();
   rf_grid_wait();
   const int len = rf_seq_len(c, b, dev_status), q_len = rf_query_len(u, b, dev_status);
   const int sees = tile < u.n_q ? rf_rows_see(u, len, q_len, tile * kPage, kPage) : -1;

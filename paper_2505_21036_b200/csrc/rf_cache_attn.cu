@@ -90,7 +90,7 @@ __device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem&
 }
 template <int kRows>
 struct TokenPlaces {
-  static constexpr int kRowsOf = kRows, kEnd = 2;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
+  static constexpr int kRowsOf = kRows, kEnd = 6;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
   static __device__ __noinline__ int of(const RfCacheAttn& a, int item) {
     const int n = item_tiles(a, cache_item<kRows>(a, item));
     return n < 0 ? 0 : n + kEnd;
@@ -122,7 +122,6 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     mbar_init_fence();
   }
   if (tid == 32 * kWarps) { prefetch_tmap(&maps.k); prefetch_tmap(&maps.v); }
-  rf_grid_trigger();
   rf_grid_wait();
   const Stretch st = stretch<TokenPlaces<kRows>, C::THREADS>(a, scratch);      // (its barriers also publish the mbarriers)
   const WaitCtx wc{abort_flag, a.dev_status};
@@ -430,7 +429,6 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
   constexpr int kRows = 8 * NB, PIECE = Cfg<D, NB>::PIECE;
   __shared__ float red[2][D / 32];
   extern __shared__ float weight[];              // [ctas]
-  rf_grid_trigger();
   rf_grid_wait();
   const int x = blockIdx.x + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y;
   const int32_t* heads = reinterpret_cast<const int32_t*>(a.ws);

@@ -208,7 +208,6 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     __syncwarp();
     tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM_COLS);
   }
-  rf_grid_trigger();
   rf_grid_wait();
   tc_fence_before();
   const Stretch st = rf_cache_attn::stretch<ChunkPlaces, kThreads>(a, reinterpret_cast<StretchScratch*>(base_ptr + C::SCRATCH));   // (has barriers)
@@ -802,7 +801,6 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
 template <int D, bool LSE>
 __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_constant__ RfCacheAttn a, int ctas) {
   using C = Cfg<D>;
-  rf_grid_trigger();
   rf_grid_wait();
   const int x = blockIdx.x + 1, j = blockIdx.y / (D / 16), c0 = blockIdx.y % (D / 16) * 4;
   const int32_t* heads = reinterpret_cast<const int32_t*>(a.ws);

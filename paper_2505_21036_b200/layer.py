@@ -85,6 +85,72 @@ class RainFusionAttention:
         return num_steps / (d + (num_steps - d) * density)
 
 
+class StreamingAttention:
+    """One attention layer of a clip that is generated chunk by chunk: K and V of the finished chunks stay in a paged 8-bit cache, and at
+    every denoising step the chunk's queries attend to them and to the chunk itself.  Policy only, as above.
+
+      layer.begin_chunk()
+      for step in range(num_steps):
+          layer(q, k, v, o, step=step, num_steps=num_steps)    # the step's K and V replace the last step's in the cache
+      # the last step's stay; further operations between chunks: fork, drop, compact
+
+    The first `dense_fraction` of the steps attend to every page; with `top_k` set, the others attend to the pages that are selected
+    for every 128 query rows (the first `keep_first` and last `keep_last` always: prompt and first frame, the chunk itself and its
+    neighbours).  Everything that varies between steps is on the device, so a step can be captured into a graph."""
+
+    def __init__(self, cache: api.KVCache, heads: int, chunk_tokens: int, causal_block: int = 0, top_k=None, keep_first: int = 0,
+                 keep_last: int = 0, dense_fraction: float = 0.1):
+        import torch
+        if not (0.0 <= dense_fraction <= 1.0):
+            raise ValueError("dense_fraction must be in [0, 1]")
+        self.cache, self.heads, self.chunk_tokens, self.causal_block = cache, heads, chunk_tokens, causal_block
+        self.top_k, self.keep_first, self.keep_last, self.dense_fraction = top_k, keep_first, keep_last, dense_fraction
+        self.base = torch.zeros_like(cache.seq_len)
+        self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        self.live = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        self.ws = api.alloc_cache_attn_workspace(cache, heads, chunk_tokens)
+        self.sched = (None if top_k is None else
+                      api.CacheSchedule.empty(cache, heads, chunk_tokens, max(1, min(cache.max_pages, keep_first + keep_last + top_k))))
+
+    def is_dense_step(self, step: int, num_steps: int) -> bool:
+        return self.top_k is None or step < int(math.ceil(self.dense_fraction * num_steps - 1e-9))
+
+    def begin_chunk(self):
+        """What the cache holds now belongs to finished chunks."""
+        self.base.copy_(self.cache.seq_len)
+
+    def __call__(self, q, k, v, o, lse=None, new_len=None, step: int = 0, num_steps: int = 1):
+        """q, o [n_seqs, heads, chunk_tokens, D], k, v [n_seqs, cache.heads, chunk_tokens, D]; new_len: int32 [n_seqs] on the device, tokens
+        that each sequence's chunk really has (None: chunk_tokens)."""
+        api.rf_cache_drop(self.cache, max_len=self.base, dev_status=self.status)
+        api.rf_cache_append(self.cache, k, v, new_len, self.status)
+        sched = None
+        if not self.is_dense_step(step, num_steps):
+            sched = self.sched
+            api.rf_cache_select(self.cache, q, sched, new_len, self.causal_block, self.keep_first, self.keep_last, self.top_k, self.status)
+        api.rf_cache_attn_fwd(self.cache, q, o, lse, sched, new_len, self.causal_block, None, self.ws, self.status)
+
+    def fork(self, parent):
+        """Every sequence b continues sequence parent[b] (int32 on the device; -1: it ends)."""
+        api.rf_cache_fork(self.cache, parent, self.status)
+
+    def drop(self, first, count):
+        """Sequence b lets go of its pages [first[b], first[b] + count[b]): a window that slides."""
+        api.rf_cache_drop(self.cache, first, count, None, self.status)
+
+    def compact(self):
+        """Pages in use move to the front of the pool; returns how many there are (on the device)."""
+        api.rf_cache_compact(self.cache, self.live, self.status)
+        return self.live
+
+    def check(self):
+        """Raises if a kernel reported an error since the last check (reads the device status word)."""
+        code = int(self.status.item())
+        if code != 0:
+            self.status.zero_()
+            raise api.RainFusionError(f"device status {code}: {api.load().rf_status_string(code).decode()}")
+
+
 class HostStagedAttention:
     """The whole path for callers whose Q, K, V and O live in (pinned) host memory: a thin wrapper over the
     library's rf_host_pipeline_* calls, which pipeline groups of heads over a copy-in stream, two alternating compute
