@@ -105,23 +105,15 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
 constexpr int kHeadWords = 4;
 __host__ __device__ __forceinline__ size_t head_floats(int ctas) { return ((size_t)ctas * kHeadWords + 63) / 64 * 64; }
 
-// Four codes of a word as two pairs of bf16: byte 1 and byte 3, byte 0 and byte 2.  A code's exponent lands eight bits too low
-// for a bf16's bias (by 2^-120, subnormal codes included, as both count their mantissa from the same place), so a product with
-// 2^120 times the page's scale, exact, makes it the stored value.  Seven integer instructions and two products for four codes.
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+// Bytes 0 and 1, bytes 2 and 3 of a word of codes as fp16 pairs.
+__device__ __forceinline__ uint32_t widen_low(uint32_t x) {
   uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(d) : "r"(x));
   return d;
 }
-__device__ __forceinline__ uint32_t widen_odd(uint32_t x) { return ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u); }
-__device__ __forceinline__ uint32_t widen_even(uint32_t x) { return ((x << 4) & 0x07f007f0u) | ((x << 8) & 0x80008000u); }
-// The factors as bf16 pairs: 2^(120 + e) for the scale 2^e, in two steps where that is past bf16's exponents (e > 7).
-struct Widen { uint32_t m1, m2; };
-__device__ __forceinline__ Widen widen_by(float scale) {
-  const int e = min(max((int)((__float_as_uint(scale) >> 23) & 255u) - 127, -100), 100);
-  const uint32_t m1 = (uint32_t)(min(e, 7) + 120 + 127) << 7, m2 = (uint32_t)(max(e - 7, 0) + 127) << 7;
-  return Widen{m1 * 0x10001u, m2 * 0x10001u};
+__device__ __forceinline__ uint32_t widen_high(uint32_t x) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(d) : "r"(x));
+  return d;
 }
-constexpr uint32_t kOne2 = 0x3f803f80u;   // m2 of e <= 7
-
 }  // namespace rf_cache_attn

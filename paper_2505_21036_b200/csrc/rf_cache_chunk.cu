@@ -9,11 +9,15 @@
 // e5m2 holds exactly: q = hi + lo exactly from 2^-6 up (2^-14 of the row's largest), and below to within 2^-14 (2^-21.8 of the largest, the
 // order of an fp32 sum's own rounding).  hi K^T + lo K^T costs what one bf16 product costs, reads half the shared memory, and nothing has
 // to be widened; the page's scale and the row's go into the softmax's factor.
-// Values: the weights have to be bf16 (they span more binades than 8 bits hold), so V is widened to bf16 (exact, see widen_odd) by four
-// warps, once for the 256 rows, and laid out in shared memory in the swizzled form that tcgen05 reads, beside the softmax.
-// (K widened as well, by the same four warps: 6650 cycles a tile instead of the softmax's 2900, twice 1450 for the two and twice 900
-// for the loads, as shared memory then carries 32 KB more a tile beside the operands' 200; 24 heads, 2040 rows, 32 896 keys, D = 128:
-// 1090 us.)
+// Values: V is widened to fp16 by four warps (one conversion a pair of codes, exact), once for the 256 rows, and laid out in shared memory in
+// the swizzled form that tcgen05 reads, beside the softmax.  A page's scale has to go into V or into the weights, as O adds up over pages:
+// V is held in units of 2^ref, ref the scale of the piece's first page, in steps upwards where a page's scale is more than 2^7 above it (O
+// is then rescaled, as for a new maximum).  That is exact for scales down to 2^-15 of it; of smaller ones the last places go (2^-25 of 2^ref,
+// which 2^24 below still is bf16's precision).  The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to
+// 2^-21 of the maximum and to 2^-31 of it in steps; a row of a million keys loses 2^-12 of its weight at most.
+// (V to bf16 in seven integer instructions and two products for four codes: 2050 cycles of the widening warps' 3470 a tile, beside the softmax
+// on the same integer pipes; 24 heads, 2040 rows, 32 896 keys, D = 128: 784 us, with the widening left out 686.  K widened as well, by the
+// same four warps: 1090.)
 // Warp roles:
 //   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
 //   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q and the codes by TMA
@@ -37,10 +41,8 @@ using rf_cache_attn::Stretch;
 using rf_cache_attn::StretchScratch;
 using rf_cache_attn::head_floats;
 using rf_cache_attn::kHeadWords;
-using rf_cache_attn::kOne2;
-using rf_cache_attn::mul_bf16x2;
-using rf_cache_attn::widen_even;
-using rf_cache_attn::widen_odd;
+using rf_cache_attn::widen_high;
+using rf_cache_attn::widen_low;
 
 constexpr int kRows = 2 * BM, kThreads = 512;
 constexpr int kPagesWarp = 8, kMmaWarp = 9, kWidenWarp = 12;
@@ -57,8 +59,10 @@ static_assert(256 * kRegsSoftmax + 128 * kRegsControl + 128 * kRegsWiden <= 6553
 #define RF_REGS_WIDEN() asm volatile("setmaxnreg.dec.sync.aligned.u32 64;")
 static_assert(kRegsSoftmax == 200 && kRegsControl == 48 && kRegsWiden == 64, "keep the macros in step");
 
-constexpr float kLazyRaise = 32.0f;                         // as in the clip kernel: see there
-constexpr float kRaise = 25.0f, kRaiseMargin = 8.0f;
+// Lazy raising of the running maximum as in the clip kernel, but within what fp16 weights hold: a weight at the maximum is 2^kTop, one that
+// exceeds it by kRaise 2^15.
+constexpr float kTop = 7.0f, kRaise = 8.0f, kRaiseMargin = 3.0f;
+constexpr int kMostUp = 7;                                  // a page's V scale above the reference, in log2
 constexpr int kSpec = 32;
 
 // TMEM columns and V's layout are those of the clip kernel (rf_attn.cu: Cfg), where they are explained: V in blocks of VBOX columns with a block of ones behind them whose product is
@@ -86,8 +90,9 @@ struct Cfg {
   static constexpr uint32_t MISC = BAR + 8 * B_COUNT;
   static constexpr uint32_t ITEM = (MISC + 16 + 15) / 16 * 16;
   static constexpr uint32_t RECORD = ITEM + kItemSlots * kItemWords * 4;    // what goes with a slot of V's codes: 4 words
-  static constexpr uint32_t FLAGS = RECORD + NS * 16;                       // a tile's flags for the MMA thread, by K slot
-  static constexpr uint32_t WINDOW = FLAGS + 16;                            // kBatch entries of the two lists, then a batch of the union
+  static constexpr uint32_t FLAGS = RECORD + NS * 16;                       // a tile's flags and V's reference for the MMA thread, by K slot
+  static constexpr uint32_t REF = FLAGS + 16;                               // V's reference of a stream's tile
+  static constexpr uint32_t WINDOW = REF + 16;                            // kBatch entries of the two lists, then a batch of the union
   static constexpr uint32_t ROWEXP = WINDOW + 4 * kBatch * 4;               // by item slot: exponent field of what undoes a row's scaling
   static_assert(ROWEXP % 8 == 0 && (ROWEXP + kItemSlots * kRows) % 8 == 0, "alignment");
   static constexpr uint32_t SCRATCH = ROWEXP + kItemSlots * kRows;
@@ -99,7 +104,7 @@ struct Cfg {
   static constexpr uint32_t P_COL0 = S_EARLY ? S_END : S_COL0, P_COL1 = S_EARLY ? S_END + 64 : S_COL1 + 64;
   static constexpr uint32_t O_COL0 = S_EARLY ? S_END + 128 : S_END, O_COL1 = O_COL0 + NPV;
   static_assert(O_COL1 + NPV <= TMEM_COLS, "TMEM columns");
-  static constexpr size_t PIECE = (size_t)(D / 4 + 1) * BM;                 // float4 of one piece of one stream: O, then {m, l, l exact, has O}
+  static constexpr size_t PIECE = (size_t)(D / 4 + 1) * BM;                 // float4 of one piece of one stream: O, then {m, l, l exact, 128 + V's reference or 0: no O}
 };
 
 // What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
@@ -131,6 +136,31 @@ struct ChunkPlaces {
   }
 };
 
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 t = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+
+// Weights of the key columns [C0, C1) of a tile as in the clip kernel, packed to fp16.
+template <int C0, int C1, bool LSE>
+__device__ __forceinline__ void take_weights_f16(const uint32_t (&s)[BN], uint32_t (&pk)[BN / 2], float2& la, float2 sc2, float2 mneg) {
+#pragma unroll
+  for (int c = C0; c < C1; c += 4) {
+    float2 e0 = __ffma2_rn(make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sc2, mneg);
+    float2 e1 = __ffma2_rn(make_float2(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), sc2, mneg);
+    e0.x = ex2(e0.x); e0.y = ex2(e0.y);
+    e1.x = ex2(e1.x); e1.y = ex2(e1.y);
+    pk[c / 2] = pack_f16(e0.x, e0.y);
+    pk[c / 2 + 1] = pack_f16(e1.x, e1.y);
+    if (LSE) la = __fadd2_rn(la, __fadd2_rn(e0, e1));
+  }
+}
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
@@ -164,7 +194,7 @@ struct Maps { CUtensorMap q, k, v; };
 template <int D, bool LSE>
 __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __grid_constant__ Maps maps, const __grid_constant__ RfCacheAttn a) {
   using C = Cfg<D>;
-  constexpr uint32_t IDESC_HI = idesc_f8(BM, BN, 0), IDESC_LO = idesc_f8(BM, BN, 1), IDESC_PV = idesc_bf16(BM, C::NPV, 1);
+  constexpr uint32_t IDESC_HI = idesc_f8(BM, BN, 0), IDESC_LO = idesc_f8(BM, BN, 1), IDESC_PV = idesc_f16(BM, C::NPV, 1);
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -173,6 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC + 8);
   int* items = reinterpret_cast<int*>(base_ptr + C::ITEM);
   volatile uint32_t* records = reinterpret_cast<volatile uint32_t*>(base_ptr + C::RECORD);
+  volatile int* refs = reinterpret_cast<volatile int*>(base_ptr + C::REF);
   volatile uint32_t* flags = reinterpret_cast<volatile uint32_t*>(base_ptr + C::FLAGS);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -185,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
 #pragma unroll 1
     for (int s = 0; s < C::NV; ++s) { mbar_init(bar(C::B_VF + s), 4); mbar_init(bar(C::B_VE + s), 1); }
     for (int j = 0; j < 2; ++j) {
-      mbar_init(bar(C::B_SF + j), 1);
+      mbar_init(bar(C::B_SF + j), 2);                        // the scores' products, and the MMA thread, which has written V's reference
       for (int p = 0; p < C::PARTS; ++p) mbar_init(bar(C::B_PF + j * C::PARTS + p), 4);
       mbar_init(bar(C::B_OF + j), 1);
       mbar_init(bar(C::B_SE + j), 4);
@@ -200,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
 #pragma unroll 1
   for (int i = tid; i < C::NV * BN * 2; i += kThreads) {   // the 16 columns behind V's: one, then zeros
     const int v = i / (BN * 2), row = i / 2 % BN, c = i % 2;
-    *reinterpret_cast<uint4*>(base_ptr + C::V0 + v * C::VTILE + C::VLOAD + C::vchunk(row, c)) = make_uint4(c == 0 ? 0x3f80u : 0u, 0u, 0u, 0u);
+    *reinterpret_cast<uint4*>(base_ptr + C::V0 + v * C::VTILE + C::VLOAD + C::vchunk(row, c)) = make_uint4(c == 0 ? 0x3c00u : 0u, 0u, 0u, 0u);
   }
   fence_proxy_async_smem();
   if (warp == kPagesWarp) {
@@ -278,7 +309,8 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       const int cs = u % C::NS, vs = u % C::NV;
       if (!__all_sync(0xffffffffu, mbar_wait(bar(C::B_CF + cs), (u / C::NS) & 1, wc))) break;
       volatile const uint32_t* r = records + cs * 4;
-      const uint32_t f = r[0], m1 = r[1], m2 = r[2];
+      const uint32_t f = r[0], factor = r[1];
+      const int valid = (int)r[2];                            // tokens of the page; behind them may lie codes of no number
       if (!(f & kMore)) break;
       if (f & kFirst) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar(C::B_QR), nq & 1, wc))) break;
@@ -295,17 +327,14 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       for (int p = 0; p < D / 16; ++p) {
         int row, c;
         widen_place<D>(p, w, lane, row, c);
-        const uint4 x = *reinterpret_cast<const uint4*>(from + C::qchunk(row, c));
+        uint4 x = *reinterpret_cast<const uint4*>(from + C::qchunk(row, c));
+        if (row >= valid) x = make_uint4(0u, 0u, 0u, 0u);
         const uint32_t* in = &x.x;
         uint32_t y[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[2 * i] = mul_bf16x2(widen_even(in[i]), m1);            // bytes 0 and 2: V's columns lie in the order 0 2 1 3 of every
-          y[2 * i + 1] = mul_bf16x2(widen_odd(in[i]), m1);         // four, and so do O's, until it is packed
-        }
-        if (m2 != kOne2) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = mul_bf16x2(y[i], m2);
+          y[2 * i] = mul_f16x2(widen_low(in[i]), factor);
+          y[2 * i + 1] = mul_f16x2(widen_high(in[i]), factor);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -353,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         ++no;
         if (e0 == b0 && e1 == b1) continue;                    // sees nothing, or lists nothing here
         bool first = true;
+        int ref = 0;
         const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
         const int32_t* l1 = l0 != nullptr && it.r0 / kPage + 1 < a.u.n_q ? l0 + a.n_k : l0;
         int i0 = b0, i1 = b1;
@@ -389,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           i0 += take0;
           i1 += take1;
           uint32_t row = 0, f = 0;
-          rf_cache_attn::Widen vw = {kOne2, kOne2};
+          int vexp = -128, valid = 0;
           if (lane < cnt) {
             const int page = win[2 * kBatch + lane];
             f = (uint32_t)win[3 * kBatch + lane] | kMore;
@@ -397,8 +427,20 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             if (lane == 0 && first) f |= kFirst;
             const int phys = rf_page(a.c, it.b, min(page, pages - 1), a.dev_status);   // (a page that no row sees: any will do)
             row = (uint32_t)phys * a.c.H + it.bh % a.c.H;
-            vw = rf_cache_attn::widen_by(a.c.v_scale[row]);
+            vexp = min(max((int)((__float_as_uint(a.c.v_scale[row]) >> 23) & 255u) - 127, -100), 100);
+            valid = min(max(it.len - page * kPage, 0), kPage);
           }
+          // V's reference: the first tile's scale, raised where a tile's is too far above it
+          int mine_ref = 0;
+#pragma unroll 1
+          for (int i = 0; i < cnt; ++i) {
+            const int e = __shfl_sync(0xffffffffu, vexp, i);
+            if ((first && i == 0) || e > ref + kMostUp) ref = e;
+            if (lane == i) mine_ref = ref;
+          }
+          const int up = vexp - mine_ref;                          // 2^up as fp16, subnormal or zero where it has to be
+          const uint32_t half = up >= -14 ? (uint32_t)(up + 15) << 10 : up >= -24 ? 1u << (up + 24) : 0u;
+          f |= (uint32_t)(mine_ref + 128) << 8;
           // the tiles one after the other, each by the lane that looked it up
 #pragma unroll 1
           for (int i = 0; i < cnt && ok; ++i, ++u) {
@@ -426,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             if (ok && u >= C::NS) ok = __all_sync(0xffffffffu, mbar_wait(bar(C::B_CE + cs), ((u / C::NS) - 1) & 1, wc));
             if (ok && lane == i) {
               volatile uint32_t* r = records + cs * 4;
-              r[0] = f; r[1] = vw.m1; r[2] = vw.m2; r[3] = slot;
+              r[0] = f; r[1] = half * 0x10001u; r[2] = (uint32_t)valid; r[3] = slot;
               mbar_expect_tx(bar(C::B_CF + cs), C::TILE);
               tma_load_3d(base + C::VS0 + cs * C::TILE, &maps.v, 0, 0, (int)row, bar(C::B_CF + cs));
             }
@@ -457,7 +499,9 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         auto desc_v = [](uint32_t lo) -> uint64_t { return ((uint64_t)DESC_HI_V << 32) | lo; };
         const uint32_t q_lo = ((base + C::Q) >> 4) | LO_KMAJOR, k_lo = ((base + C::K0) >> 4) | LO_KMAJOR;
         const uint32_t v_lo = ((base + C::V0) >> 4) | LO_VMAJOR;
-        auto issue_s = [&](int j, int ks) {
+        auto issue_s = [&](int j, int ks, uint32_t rec) {
+          refs[j] = (int)(rec >> 8) - 128;
+          mbar_arrive(bar(C::B_SF + j));
           uint32_t a0 = q_lo + 2 * j * (C::TILE >> 4);
           const uint32_t b0 = k_lo + ks * (C::TILE >> 4);
           asm volatile("" : "+r"(a0));
@@ -504,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           tc_fence_after();
 #pragma unroll 1
           for (int j = 0; j < 2; ++j)
-            if (rec & (1 << j)) { s_free(j); issue_s(j, u % C::NK); }
+            if (rec & (1 << j)) { s_free(j); issue_s(j, u % C::NK, rec); }
           tc_commit(bar(C::B_KE + u % C::NK));
           if (rec & kLast) tc_commit(bar(C::B_QE));
         };
@@ -536,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             if constexpr (C::S_EARLY) {
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks); }
+                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks, nxt); }
                 if (cur & (1 << j)) {
                   issue_pv(j, vs, (acc >> j) & 1, (pv_par >> j) & 1);
                   acc |= 1u << j;
@@ -551,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
                   acc |= 1u << j;
                   pv_par ^= 1u << j;
                 }
-                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks); }
+                if (nxt & (1 << j)) { s_free(j); issue_s(j, ks, nxt); }
               }
             }
             tc_commit(bar(C::B_KE + ks));
@@ -585,6 +629,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       if (r < a.u.rows && r % a.u.M < iw[3]) sees = rf_row_sees(a.u.causal, iw[2], iw[3], r % a.u.M);
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)iw[0] * a.u.n_q + min(iw[1] / kPage + j, a.u.n_q - 1)) * a.n_k : nullptr;
       float m_run = -INFINITY, l_run = 0.f, l_exact = 0.f;
+      int ref_run = 0;                                    // O is in units of 2^ref_run
       // The factor of a tile's scores holds the page's scale: the page is looked up two tiles ahead, its scale one.
       const int32_t* table = a.c.table + (size_t)(iw[0] / a.c.H) * a.c.max_pages;
       const float* k_scale = a.c.k_scale + iw[0] % a.c.H;
@@ -620,6 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         const bool partial = __any_sync(0xffffffffu, left < BN);
         mbar_wait(bar(C::B_SF + j), done & 1, wc);
         tc_fence_after();
+        const int ref = refs[j];
         uint32_t s[128];
         uint32_t l_tile;
         if constexpr (!C::S_EARLY) l_tile = tmem_ld1(t_o + D);
@@ -643,8 +689,8 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             mx1 = fmaxf(mx1, fmaxf(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])));
           }
           const float m_tile = fmaxf(mx0, mx1) * sc;
-          const bool raise = m_tile > m_run + kLazyRaise || (m_run == -INFINITY && m_tile > -INFINITY);
-          const bool any_raise = __any_sync(0xffffffffu, raise);
+          const bool raise = m_tile > m_run + kRaise || (m_run == -INFINITY && m_tile > -INFINITY);
+          const bool any_raise = __any_sync(0xffffffffu, raise || ref != ref_run);
           float alpha = 1.f;
           if (raise) {
             alpha = ex2(m_run - m_tile);
@@ -656,13 +702,14 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           if (!opens && any_raise) {
             mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
             o_landed = true;
-            rescale_o<D>(t_o, alpha);
+            rescale_o<D>(t_o, alpha * pow2i(ref_run - ref));
           }
+          ref_run = ref;
           const float m_use = m_run == -INFINITY ? 0.f : m_run;
-          const float2 sc2 = make_float2(sc, sc), mneg = make_float2(-m_use, -m_use);
+          const float2 sc2 = make_float2(sc, sc), mneg = make_float2(kTop - m_use, kTop - m_use);
           float2 la = make_float2(0.f, 0.f);
           uint32_t pk[64];
-          take_weights<0, BN, LSE>(s, pk, la, sc2, mneg);
+          take_weights_f16<0, BN, LSE>(s, pk, la, sc2, mneg);
           if (LSE) l_exact += la.x + la.y;
           if (!o_landed) mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
           tc_fence_after();
@@ -687,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         float2 la = make_float2(0.f, 0.f);
         const float2 sc2 = make_float2(sc, sc);
         float m_use = m_run == -INFINITY ? 0.f : m_run;
-        take_weights<0, kSpec, LSE>(s, pk, la, sc2, make_float2(-m_use, -m_use));
+        take_weights_f16<0, kSpec, LSE>(s, pk, la, sc2, make_float2(kTop - m_use, kTop - m_use));
         float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
         for (int c = 0; c < 128; c += 4) {
@@ -695,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           mx1 = fmaxf(mx1, fmaxf(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])));
         }
         const float m_tile = fmaxf(mx0, mx1) * sc;
-        if (__any_sync(0xffffffffu, m_tile > m_run + kRaise)) {
+        if (__any_sync(0xffffffffu, m_tile > m_run + kRaise || ref != ref_run)) {
           float alpha = 1.f;
           if (m_tile > m_run + kRaiseMargin) {
             alpha = ex2(m_run - m_tile);
@@ -705,23 +752,24 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           }
           if (!opens) {
             mbar_wait(bar(C::B_OF + j), (done - 1) & 1, wc);
-            rescale_o_call<D>(t_o, alpha);
+            rescale_o_call<D>(t_o, alpha * pow2i(ref_run - ref));
           }
+          ref_run = ref;
           m_use = m_run == -INFINITY ? 0.f : m_run;
           la = make_float2(0.f, 0.f);
-          take_weights<0, kSpec, LSE>(s, pk, la, sc2, make_float2(-m_use, -m_use));
+          take_weights_f16<0, kSpec, LSE>(s, pk, la, sc2, make_float2(kTop - m_use, kTop - m_use));
         }
         const uint32_t t_p = tmem_base + lane_sel + (j ? C::P_COL1 : C::P_COL0);
-        const float2 mneg = make_float2(-m_use, -m_use);
-        take_weights<kSpec, 64, LSE>(s, pk, la, sc2, mneg);
+        const float2 mneg = make_float2(kTop - m_use, kTop - m_use);
+        take_weights_f16<kSpec, 64, LSE>(s, pk, la, sc2, mneg);
         store_weights<0, 64>(t_p, pk);
         tmem_st1(t_o + D, 0u);
-        take_weights<64, 80, LSE>(s, pk, la, sc2, mneg);
+        take_weights_f16<64, 80, LSE>(s, pk, la, sc2, mneg);
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::B_PF + j * C::PARTS));
-        take_weights<80, BN, LSE>(s, pk, la, sc2, mneg);
+        take_weights_f16<80, BN, LSE>(s, pk, la, sc2, mneg);
         store_weights<64, BN>(t_p, pk);
         tc_wait_st();
         tc_fence_before();
@@ -752,13 +800,13 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
                                                           __uint_as_float(v[4 * i + 3])));
           }
         }
-        __stcg(mine + (D / 4) * BM, make_float4(m_run, l_run, l_exact, n > 0 ? 1.f : 0.f));
+        __stcg(mine + (D / 4) * BM, make_float4(m_run, l_run, l_exact, n > 0 ? (float)(ref_run + 128) : 0.f));
       } else {
         const bool there = r < a.u.rows && r % a.u.M < iw[3];
         const size_t at_row = (size_t)iw[0] * a.u.rows + min(r, a.u.rows - 1);
         uint4* o = reinterpret_cast<uint4*>(a.o + at_row * D);
         const bool o32 = (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0;
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+        const float inv = l_run == 0.f ? 0.f : pow2i(ref_run) / l_run;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -771,16 +819,11 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           }
           if (there) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {                  // columns 0 2 1 3 of every four
-              const float x0 = __uint_as_float(v[4 * i]) * inv, x2 = __uint_as_float(v[4 * i + 1]) * inv;
-              const float x1 = __uint_as_float(v[4 * i + 2]) * inv, x3 = __uint_as_float(v[4 * i + 3]) * inv;
-              v[2 * i] = pack_bf16(x0, x1);
-              v[2 * i + 1] = pack_bf16(x2, x3);
-            }
+            for (int i = 0; i < 16; ++i) v[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
             store_columns(o + c * 4, v, o32);
           }
         }
-        if (LSE && there) a.lse[at_row] = (m_run + log2f(l_exact)) * 0.6931471805599453f;
+        if (LSE && there) a.lse[at_row] = (m_run - kTop + log2f(l_exact)) * 0.6931471805599453f;
       }
       tc_fence_before();
       __syncwarp();
@@ -815,6 +858,7 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   if (row >= a.u.rows || row % a.u.M >= it.q_len) return;
   const float4* pieces = reinterpret_cast<const float4*>(a.ws + head_floats(ctas)) + threadIdx.x;
   float m = -INFINITY, l = 0.f, lx = 0.f;
+  int ref = -128;
   float4 acc[4] = {};
 #pragma unroll 1
   for (int i = 0; i <= n; ++i) {
@@ -833,6 +877,10 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
     }
     l = l * keep + st.y * w;
     lx = lx * keep + st.z * w;
+    const int mine_ref = (int)st.w - 128, top = max(ref, mine_ref);
+    keep *= pow2i(ref - top);
+    w *= pow2i(mine_ref - top);
+    ref = top;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       acc[k].x = acc[k].x * keep + o[k].x * w;
@@ -841,16 +889,16 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
       acc[k].w = acc[k].w * keep + o[k].w * w;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = l == 0.f ? 0.f : pow2i(ref) / l;
   uint32_t v[8];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    v[2 * k] = pack_bf16(acc[k].x * inv, acc[k].z * inv);        // columns 0 2 1 3 of every four
-    v[2 * k + 1] = pack_bf16(acc[k].y * inv, acc[k].w * inv);
+    v[2 * k] = pack_bf16(acc[k].x * inv, acc[k].y * inv);
+    v[2 * k + 1] = pack_bf16(acc[k].z * inv, acc[k].w * inv);
   }
   const size_t at_row = (size_t)it.bh * a.u.rows + row;
   store_sector(reinterpret_cast<uint4*>(a.o + at_row * D) + c0 / 2, v, (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0);
-  if (LSE && c0 == 0) a.lse[at_row] = (m + log2f(lx)) * 0.6931471805599453f;
+  if (LSE && c0 == 0) a.lse[at_row] = (m - kTop + log2f(lx)) * 0.6931471805599453f;
 }
 
 int chunk_ctas(const RfCache& c, const RfQueries& u) {
