@@ -485,9 +485,10 @@ __global__ void __launch_bounds__(256) rf_cache_move_kernel(RfCache c, const int
 // ------------------------------------------------------------------------------------------------ select
 // A CTA takes up to 8 tiles of query rows of a K/V head: their sums, their products with every page's key sum, the top_k best of each,
 // the lists in order.  Scores are in 64 bits: a page's place must not hang on the order of a summation, and two scores that differ in
-// exact arithmetic hardly ever agree to 1e-16.  What bounds it: widening the key sums to 64 bits (16 a cycle and SM), so a lane takes a
-// page, widens its D numbers once and multiplies them with all of the CTA's tiles; a tile's own pass per CTA was 136 us for 29
-// tiles x 931 pages x 24 heads, 83 us for a token each of 32 heads.
+// exact arithmetic hardly ever agree to 1e-16.  What bounds it: widening the key sums to 64 bits (16 a cycle and SM) and the 64-bit
+// products, so the tiles are the columns and the pages the rows of a 64-bit matrix product: a lane widens a number once for eight tiles and
+// holds its part of the tiles' sums in registers.  (29 tiles x 931 pages x 24 heads: 136 us with a tile a CTA, 67 with a lane a page and
+// four tiles a CTA, whose loads touched 32 rows at a time.)
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 
 __device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below everything
@@ -496,13 +497,18 @@ __device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below
   return u >> 63 ? ~u : u | (1ull << 63);
 }
 
+// D (8 pages x 8 tiles) += A (8 x 4) B (4 x 8): a lane holds A[lane / 4][lane % 4], B[lane % 4][lane / 4], D[lane / 4][2 (lane % 4) + 0, 1].
+__device__ __forceinline__ void mma_f64(double (&d)[2], double a, double b) {
+  asm volatile("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(d[0]), "+d"(d[1]) : "d"(a), "d"(b));
+}
+
 template <int D, int T>
-__global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c, RfQueries u, int keep_first, int keep_last, int top_k, int32_t* count,
+__global__ void __launch_bounds__(kSelThreads, 1) rf_cache_select_kernel(RfCache c, RfQueries u, int keep_first, int keep_last, int top_k, int32_t* count,
                                                                       int32_t* pages, int n_k, int32_t* dev_status) {
   constexpr int kOf = kSelWarps / T, kTeam = 32 * kOf;     // warps and threads that work on a tile
   extern __shared__ uint64_t keys[];                       // [T][pages of the sequence]
   __shared__ double part[kSelWarps][D];
-  __shared__ __align__(16) double pooled[D][T];
+  __shared__ double pooled[T][D];
   __shared__ __align__(16) float tail_sum[D];
   __shared__ int hist[T][256], state[T][4], warp_n[kSelWarps][2], cand[T + 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -526,19 +532,38 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
   int equal_allowed = 0;                                    // pages of exactly the threshold's score that are taken, lowest first
   if (most > 0) {                                           // (the same for the whole CTA)
     {
-      // the sums of the tile's rows, a lane every 32nd column, a warp every kOf-th row
-      double acc[D / 32] = {};
-      const __nv_bfloat16* q = u.q + (((size_t)b * c.H + h) * u.rows + (size_t)tile * kPage) * D + lane;
+      // the sums of the tile's rows: a lane's columns (two, four, or at D = 96 every 32nd), a warp every kOf-th row, eight of them under way
+      constexpr int kMine = D / 32, kAhead = 8;
+      auto column = [&](int i) { return D == 96 ? lane + 32 * i : lane * kMine + i; };
+      double acc[kMine] = {};
+      const __nv_bfloat16* q = u.q + (((size_t)b * c.H + h) * u.rows + (size_t)tile * kPage) * D;
       const int rows = scored ? min(kPage, u.rows - tile * kPage) : 0;
-#pragma unroll 4
-      for (int r = wrank; r < rows; r += kOf) {
-        const int at = tile * kPage + r;
-        if ((u.G == 1 ? at : at % u.M) >= q_len) continue;
+#pragma unroll 1
+      for (int r0 = wrank; r0 < rows; r0 += kOf * kAhead) {
+        uint16_t v[kAhead][kMine];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] += (double)__bfloat162float(q[(size_t)r * D + 32 * i]);
+        for (int k = 0; k < kAhead; ++k) {
+          const int r = r0 + k * kOf, at = tile * kPage + r;
+          const bool there = r < rows && (u.G == 1 ? at : at % u.M) < q_len;
+          const __nv_bfloat16* x = q + (size_t)(there ? r : 0) * D;
+          if (D == 128) {
+            const uint2 t = there ? *reinterpret_cast<const uint2*>(x + lane * 4) : make_uint2(0u, 0u);
+            v[k][0] = (uint16_t)t.x; v[k][1] = (uint16_t)(t.x >> 16); v[k][kMine - 2] = (uint16_t)t.y; v[k][kMine - 1] = (uint16_t)(t.y >> 16);
+          } else if (D == 64) {
+            const uint32_t t = there ? *reinterpret_cast<const uint32_t*>(x + lane * 2) : 0u;
+            v[k][0] = (uint16_t)t; v[k][1] = (uint16_t)(t >> 16);
+          } else {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) v[k][i] = there ? *reinterpret_cast<const uint16_t*>(x + column(i)) : (uint16_t)0;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) acc[i] += (double)__uint_as_float((uint32_t)v[k][i] << 16);
       }
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) part[warp][lane + 32 * i] = acc[i];
+      for (int i = 0; i < kMine; ++i) part[warp][column(i)] = acc[i];
     }
     // A last page that is not full is summed up from its codes: it may be part of a page that another sequence has filled
     // further, or that was fuller when it was written.
@@ -558,32 +583,36 @@ __global__ void __launch_bounds__(kSelThreads) rf_cache_select_kernel(RfCache c,
       double x = 0.0;
 #pragma unroll
       for (int k = 0; k < kOf; ++k) x += part[t * kOf + k][d];
-      pooled[d][t] = x;
+      pooled[t][d] = x;
     }
     __syncthreads();
+    // four columns of every 16 for a lane, so that it reads 16 bytes at a time: a sum's order is free
+    const int g = lane >> 2, q4 = lane & 3;
+    double w[D / 16][4];
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[d][k] = g < T ? pooled[g < T ? g : 0][16 * d + 4 * q4 + k] : 0.0;
 #pragma unroll 1
-    for (int c0 = keep_first + warp * 32; c0 < most; c0 += kSelThreads) {
-      const int col = c0 + lane;
+    for (int c0 = keep_first + warp * 8; c0 < most; c0 += kSelWarps * 8) {
+      const int col = c0 + g;
       const bool there = col < most;
-      const float4* x = reinterpret_cast<const float4*>(col == tail ? tail_sum : c.k_sum + ((size_t)(there ? rf_page(c, b, col, dev_status) : 0) * c.H + h) * D);
-      double dot[T] = {};
-#pragma unroll 4
-      for (int d = 0; d < D; d += 4) {
-        const float4 v = there ? x[d / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float f[4] = {v.x, v.y, v.z, v.w};
+      const float4* x = reinterpret_cast<const float4*>(col == tail ? tail_sum : c.k_sum + ((size_t)(there ? rf_page(c, b, col, dev_status) : 0) * c.H + h) * D) + q4;
+      float4 v[D / 16];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const double w = (double)f[k];
+      for (int d = 0; d < D / 16; ++d) v[d] = there ? x[4 * d] : make_float4(0.f, 0.f, 0.f, 0.f);
+      double dot[2] = {};
 #pragma unroll
-          for (int t = 0; t < T; ++t) dot[t] += pooled[d + k][t] * w;
-        }
+      for (int d = 0; d < D / 16; ++d) {
+        mma_f64(dot, (double)v[d].x, w[d][0]);
+        mma_f64(dot, (double)v[d].y, w[d][1]);
+        mma_f64(dot, (double)v[d].z, w[d][2]);
+        mma_f64(dot, (double)v[d].w, w[d][3]);
       }
-      if (there) {
-        const double tokens = (double)min(kPage, len - col * kPage);
+      const double tokens = (double)min(kPage, len - col * kPage);
 #pragma unroll
-        for (int t = 0; t < T; ++t)
-          if (col < cand[t]) keys[(size_t)t * c.max_pages + col] = ordered(dot[t] / tokens);
-      }
+      for (int i = 0; i < 2; ++i)
+        if (2 * q4 + i < T && there && col < cand[2 * q4 + i < T ? 2 * q4 + i : 0]) keys[(size_t)(2 * q4 + i) * c.max_pages + col] = ordered(dot[i] / tokens);
     }
     __syncthreads();
   }
@@ -747,19 +776,18 @@ cudaError_t rf_launch_cache_compact(const RfCache& c, int32_t* n_live, int32_t* 
 
 cudaError_t rf_launch_cache_select(const RfCache& c, const RfQueries& u, int keep_first, int keep_last, int top_k, int32_t* count,
                                    int32_t* pages, int n_k, int32_t* dev_status, cudaStream_t st) {
-  // Four tiles a CTA share the widening of the key sums; one where the scores of four do not fit in shared memory or there are no
-  // four tiles.
-  const bool four = u.n_q >= 4 && 4 * sizeof(uint64_t) * (size_t)c.max_pages <= 128 * 1024;
-  const size_t smem = (four ? 4 : 1) * sizeof(uint64_t) * (size_t)c.max_pages;
+  // Eight tiles a CTA share the key sums; one where the scores of eight do not fit in shared memory or there is only one.
+  const bool eight = u.n_q > 1 && 8 * sizeof(uint64_t) * (size_t)c.max_pages <= 128 * 1024;
+  const size_t smem = (eight ? 8 : 1) * sizeof(uint64_t) * (size_t)c.max_pages;
   auto go = [&](auto kernel, bool (&done)[64]) -> cudaError_t {
     const cudaError_t e = allow_smem(kernel, smem + 48 * 1024, done);   // (the static arrays count too)
     if (e != cudaSuccess) return e;
-    return rf_launch(kernel, dim3(rf_cdiv(u.n_q, four ? 4 : 1), c.H, c.B), kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
+    return rf_launch(kernel, dim3(rf_cdiv(u.n_q, eight ? 8 : 1), c.H, c.B), kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
   };
   static bool done[6][64] = {};
   switch (c.D) {
-    case 64: return four ? go(rf_cache_select_kernel<64, 4>, done[0]) : go(rf_cache_select_kernel<64, 1>, done[1]);
-    case 96: return four ? go(rf_cache_select_kernel<96, 4>, done[2]) : go(rf_cache_select_kernel<96, 1>, done[3]);
-    default: return four ? go(rf_cache_select_kernel<128, 4>, done[4]) : go(rf_cache_select_kernel<128, 1>, done[5]);
+    case 64: return eight ? go(rf_cache_select_kernel<64, 8>, done[0]) : go(rf_cache_select_kernel<64, 1>, done[1]);
+    case 96: return eight ? go(rf_cache_select_kernel<96, 8>, done[2]) : go(rf_cache_select_kernel<96, 1>, done[3]);
+    default: return eight ? go(rf_cache_select_kernel<128, 8>, done[4]) : go(rf_cache_select_kernel<128, 1>, done[5]);
   }
 }
