@@ -397,7 +397,7 @@ def _cache_arg(name, t, dtype, shape, device):
     """The caller's tensor, checked: the kernels index it as a contiguous array of this type and shape."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise RainFusionError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is wanted, got {t.dtype} {tuple(t.shape)} "
                               f"{'' if t.is_contiguous() else 'not contiguous '}on {t.device}")
     return t.data_ptr()
@@ -425,6 +425,12 @@ class KVCache:
         self.page_table, self.seq_len, self.device = page_table, seq_len, dev
         self.n_seqs, self.heads, self.D, self.n_pages, self.max_pages = n_seqs, heads, D, n_pages, max_pages
         self.ref = C.byref(self.c)
+        # what every call asks for, looked up once (a call's host time counts where its kernels take ten microseconds)
+        self._int32, self._bf16, self._float = torch.int32, torch.bfloat16, torch.float32
+        self._per_seq, self._one = (n_seqs,), (1,)
+        self._current_device = torch.cuda.current_device
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self._queries = {}
         n = load().rf_cache_workspace_bytes(self.ref)
         if n == 0:
             raise RainFusionError("rf_cache_workspace_bytes: unsupported sizes or misaligned tensors")
@@ -439,17 +445,33 @@ class KVCache:
         return cls(k, torch.empty_like(k), torch.empty((n_pages, heads), **f), torch.empty((n_pages, heads), **f),
                    torch.empty((n_pages, heads, D), **f), torch.zeros((n_seqs, max_pages), **i), torch.zeros((n_seqs,), **i))
 
-    def ints(self, name, t, n=None):
-        """A device int32 argument [n_seqs] (or [n]); None stays None."""
-        import torch
-        return _cache_arg(name, t, torch.int32, (self.n_seqs if n is None else n,), self.device)
+    def ints(self, name, t):
+        """A device int32 argument [n_seqs]; None stays None."""
+        return None if t is None else _cache_arg(name, t, self._int32, self._per_seq, self.device)
+
+    def word(self, name, t):
+        """A device int32 argument [1]; None stays None."""
+        return None if t is None else _cache_arg(name, t, self._int32, self._one, self.device)
 
     def stream(self):
         """The current stream, which has to be the cache's device's."""
-        import torch
-        if self.device.index != torch.cuda.current_device():
-            raise RainFusionError(f"the cache is on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
-        return _stream()
+        now = self._current_device()
+        if self.device.index != now:
+            raise RainFusionError(f"the cache is on {self.device}, the current device is cuda:{now}")
+        return _stream() if self._raw_stream is None else self._raw_stream(now) or None
+
+    def query(self, q, causal_block, scale):
+        """The address of q [n_seqs, H, M, D] and the rf_cache_query that goes with its sizes."""
+        if q.dim() != 4:
+            raise RainFusionError("q: [n_seqs, H, M, D] is wanted")
+        H, M = q.shape[1], q.shape[2]
+        ptr = _cache_arg("q", q, self._bf16, (self.n_seqs, H, M, self.D), self.device)
+        key = (H, M, causal_block, scale)
+        if key not in self._queries:
+            if len(self._queries) >= 64:
+                self._queries.clear()
+            self._queries[key] = C.byref(rf_cache_query(H, M, causal_block, 0.0 if scale is None else scale))
+        return ptr, self._queries[key]
 
 
 class CacheSchedule:
@@ -483,57 +505,50 @@ def alloc_cache_attn_workspace(cache: KVCache, H: int, M: int):
 
 def rf_cache_append(cache: KVCache, k, v, new_len=None, dev_status=None):
     """k, v: bf16 [n_seqs, heads, M, D]; new_len: int32 [n_seqs] on the device, or None for M tokens everywhere."""
-    import torch
-    shape = (cache.n_seqs, cache.heads, k.shape[2] if k.dim() == 4 else -1, cache.D)
-    _check(load().rf_cache_append(cache.ref, _cache_arg("k", k, torch.bfloat16, shape, cache.device),
-                                  _cache_arg("v", v, torch.bfloat16, shape, cache.device), shape[2], cache.ints("new_len", new_len),
-                                  cache.ws.data_ptr(), cache.ws.numel(), cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_append")
+    M = k.shape[2] if k.dim() == 4 else -1
+    shape = (cache.n_seqs, cache.heads, M, cache.D)
+    _check(load().rf_cache_append(cache.ref, _cache_arg("k", k, cache._bf16, shape, cache.device), _cache_arg("v", v, cache._bf16, shape, cache.device),
+                                  M, cache.ints("new_len", new_len), cache.ws.data_ptr(), cache.ws.numel(), cache.word("dev_status", dev_status),
+                                  cache.stream()), "rf_cache_append")
 
 
 def rf_cache_fork(cache: KVCache, parent, dev_status=None):
-    _check(load().rf_cache_fork(cache.ref, cache.ints("parent", parent), cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_fork")
+    _check(load().rf_cache_fork(cache.ref, cache.ints("parent", parent), cache.word("dev_status", dev_status), cache.stream()), "rf_cache_fork")
 
 
 def rf_cache_drop(cache: KVCache, first=None, count=None, max_len=None, dev_status=None):
     _check(load().rf_cache_drop(cache.ref, cache.ints("first", first), cache.ints("count", count), cache.ints("max_len", max_len),
-                                cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_drop")
+                                cache.word("dev_status", dev_status), cache.stream()), "rf_cache_drop")
 
 
 def rf_cache_compact(cache: KVCache, n_live, dev_status=None):
-    _check(load().rf_cache_compact(cache.ref, cache.ints("n_live", n_live, 1), cache.ws.data_ptr(), cache.ws.numel(),
-                                   cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_compact")
+    _check(load().rf_cache_compact(cache.ref, cache.word("n_live", n_live), cache.ws.data_ptr(), cache.ws.numel(),
+                                   cache.word("dev_status", dev_status), cache.stream()), "rf_cache_compact")
 
 
-def _cache_query(cache, q, causal_block, scale):
-    import torch
-    if q.dim() != 4:
-        raise RainFusionError("q: [n_seqs, H, M, D] is wanted")
-    return (_cache_arg("q", q, torch.bfloat16, (cache.n_seqs, q.shape[1], q.shape[2], cache.D), cache.device),
-            rf_cache_query(q.shape[1], q.shape[2], causal_block, 0.0 if scale is None else scale))
+def _cache_sched(cache, sched):
+    if sched.pages.shape[0] != cache.n_seqs or sched.pages.shape[1] != cache.heads or sched.pages.device != cache.device:
+        raise RainFusionError("the schedule was not made for this cache")
+    return sched.ref
 
 
 def rf_cache_select(cache: KVCache, q, sched: CacheSchedule, q_len=None, causal_block=0, keep_first=0, keep_last=0, top_k=0, dev_status=None):
     """Fills sched with the pages that the tiles of query rows of q [n_seqs, H, M, D] attend to."""
-    ptr, query = _cache_query(cache, q, causal_block, None)
-    if tuple(sched.pages.shape[:2]) != (cache.n_seqs, cache.heads) or sched.pages.device != cache.device:
-        raise RainFusionError("the schedule was not made for this cache")
-    _check(load().rf_cache_select(cache.ref, C.byref(query), ptr, cache.ints("q_len", q_len), keep_first, keep_last, top_k, sched.ref,
-                                  cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_select")
+    ptr, query = cache.query(q, causal_block, None)
+    _check(load().rf_cache_select(cache.ref, query, ptr, cache.ints("q_len", q_len), keep_first, keep_last, top_k, _cache_sched(cache, sched),
+                                  cache.word("dev_status", dev_status), cache.stream()), "rf_cache_select")
 
 
 def rf_cache_attn_fwd(cache: KVCache, q, o, lse=None, sched: Optional[CacheSchedule] = None, q_len=None, causal_block=0, scale=None, ws=None,
                       dev_status=None):
     """q, o: bf16 [n_seqs, H, M, D]; lse: float [n_seqs, H, M] or None; ws: alloc_cache_attn_workspace(cache, H, M), by default a block
     from torch's allocator for the time of the call."""
-    import torch
-    ptr, query = _cache_query(cache, q, causal_block, scale)
+    ptr, query = cache.query(q, causal_block, scale)
     if ws is None:
         ws = alloc_cache_attn_workspace(cache, q.shape[1], q.shape[2])
     if ws.device != cache.device:
         raise RainFusionError("ws is not on the cache's device")
-    if sched is not None and (tuple(sched.pages.shape[:2]) != (cache.n_seqs, cache.heads) or sched.pages.device != cache.device):
-        raise RainFusionError("the schedule was not made for this cache")
-    _check(load().rf_cache_attn_fwd(cache.ref, C.byref(query), ptr, cache.ints("q_len", q_len), None if sched is None else sched.ref,
-                                    _cache_arg("o", o, torch.bfloat16, q.shape, cache.device),
-                                    _cache_arg("lse", lse, torch.float32, q.shape[:3], cache.device), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                    cache.ints("dev_status", dev_status, 1), cache.stream()), "rf_cache_attn_fwd")
+    _check(load().rf_cache_attn_fwd(cache.ref, query, ptr, cache.ints("q_len", q_len), None if sched is None else _cache_sched(cache, sched),
+                                    _cache_arg("o", o, cache._bf16, q.shape, cache.device),
+                                    _cache_arg("lse", lse, cache._float, q.shape[:3], cache.device), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                    cache.word("dev_status", dev_status), cache.stream()), "rf_cache_attn_fwd")
