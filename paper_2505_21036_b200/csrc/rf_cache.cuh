@@ -53,8 +53,9 @@ __device__ __forceinline__ int rf_row_sees(int causal, int len, int q_len, int i
 // (Out of line: two divisions, and its callers' code is to stay short.)  The most keys that any of the rows [r0, r0 + n) of a K/V head sees (they grow with a row's place in its head); -1 if
 // all of them are padding.  Row r is row r % M of its query head.
 static __device__ __noinline__ int rf_rows_see(const RfQueries& u, int len, int q_len, int r0, int n) {
-  const int i0 = r0 % u.M, end = i0 + min(n, u.rows - r0);
-  int last;                                        // the last place in a head among the rows that are there
+  int i0 = r0, last;                               // the last place in a head among the rows that are there
+  if (u.G != 1) i0 = r0 % u.M;
+  const int end = i0 + min(n, u.rows - r0);
   if (end <= u.M) last = i0 < q_len ? min(end, q_len) - 1 : -1;
   else last = i0 < q_len || end >= u.M + q_len ? q_len - 1 : end - u.M - 1;
   return last < 0 ? -1 : rf_row_sees(u.causal, len, q_len, last);

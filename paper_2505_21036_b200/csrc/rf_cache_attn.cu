@@ -72,16 +72,21 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   return d;
 }
 
-// Key tiles that an item walks; -1: all of its rows are padding.
-__device__ __forceinline__ int item_tiles(const RfCacheAttn& a, const CacheItem& it) {
-  if (it.sees < 0) return -1;
-  return a.count == nullptr ? rf_pages(it.sees) : listed(a, it, it.r0 / kPage);
+// An item and the key tiles that it walks; -1: all of its rows are padding.
+struct TokenItem { CacheItem it; int tiles; };
+template <int kRows>
+static __device__ __noinline__ TokenItem token_item(const RfCacheAttn& a, int item) {
+  TokenItem t;
+  t.it = cache_item<kRows>(a, item);
+  const int sees = rf_rows_see(a.u, t.it.len, t.it.q_len, t.it.r0, kRows);
+  t.tiles = sees < 0 ? -1 : a.count == nullptr ? rf_pages(sees) : listed(a, t.it, t.it.r0 / kPage);
+  return t;
 }
 template <int kRows>
 struct TokenPlaces {
   static constexpr int kRowsOf = kRows, kEnd = 6;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
-  static __device__ __noinline__ int of(const RfCacheAttn& a, int item) {
-    const int n = item_tiles(a, cache_item<kRows>(a, item));
+  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+    const int n = token_item<kRows>(a, item).tiles;
     return n < 0 ? 0 : n + kEnd;
   }
 };
@@ -141,8 +146,9 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     };
 #pragma unroll 1
     for (long long pos = st.lo; pos < st.hi; ++item) {
-      const CacheItem it = cache_item<kRows>(a, item);
-      const int tiles = item_tiles(a, it);
+      const TokenItem ti = token_item<kRows>(a, item);
+      const CacheItem it = ti.it;
+      const int tiles = ti.tiles;
       if (tiles < 0) continue;
       const int n = max(tiles, 1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
       at += tiles + TokenPlaces<kRows>::kEnd;
@@ -218,7 +224,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       }
       if (rec.flags & kEnd) break;
       if (rec.flags & kFirst) {
-        it = cache_item<kRows>(a, rec.item);
+        it = token_item<kRows>(a, rec.item).it;
         const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
         int row_sees = -1;                                         // keys that row `lane` sees; -1: it is not there
         if (lane < kRows && it.r0 + lane < a.u.rows) {

@@ -28,9 +28,9 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const sm
 }
 
 // An item: rows [r0, r0 + kRows) of K/V head bh.
-struct CacheItem { int b, bh, r0, len, q_len, sees; };
+struct CacheItem { int b, bh, r0, len, q_len; };
 template <int kRows>
-static __device__ __noinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
+__device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
   const int blocks = rf_cdiv(a.u.rows, kRows);
   CacheItem it;
   it.bh = item / blocks;
@@ -38,7 +38,6 @@ static __device__ __noinline__ CacheItem cache_item(const RfCacheAttn& a, int it
   it.b = it.bh / a.c.H;
   it.len = rf_seq_len(a.c, it.b, a.dev_status);
   it.q_len = rf_query_len(a.u, it.b, a.dev_status);
-  it.sees = rf_rows_see(a.u, it.len, it.q_len, it.r0, kRows);
   return it;
 }
 // Entries of the list of a tile of query rows.

@@ -110,29 +110,29 @@ struct Cfg {
 // What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
 constexpr int kItemPlaces = 6;
 
-// The two streams' lists of an item: how long they are, how many keys their rows see at most.
-struct Streams { int n0, n1, sees0, sees1; };
-static __device__ __noinline__ Streams streams(const RfCacheAttn& a, const CacheItem& it) {
-  Streams s;
-  const int tile = it.r0 / kPage;
-  s.sees0 = rf_rows_see(a.u, it.len, it.q_len, it.r0, BM);
-  s.sees1 = it.r0 + BM < a.u.rows ? rf_rows_see(a.u, it.len, it.q_len, it.r0 + BM, BM) : -1;
-  if (a.count == nullptr) {
-    s.n0 = rf_pages(max(s.sees0, 0));
-    s.n1 = rf_pages(max(s.sees1, 0));
-  } else {
-    s.n0 = s.sees0 < 0 ? 0 : rf_cache_attn::listed(a, it, tile);
-    s.n1 = s.sees1 < 0 ? 0 : rf_cache_attn::listed(a, it, tile + 1);
+// An item and the two streams' lists: how long they are.  there: some row is no padding.
+struct ChunkItem { CacheItem it; int n0, n1; bool there; };
+static __device__ __noinline__ ChunkItem chunk_item(const RfCacheAttn& a, int item) {
+  ChunkItem c;
+  c.it = rf_cache_attn::cache_item<kRows>(a, item);
+  int n[2];
+  c.there = false;
+#pragma unroll 1
+  for (int j = 0; j < 2; ++j) {
+    const int r = c.it.r0 + j * BM, sees = r < a.u.rows ? rf_rows_see(a.u, c.it.len, c.it.q_len, r, BM) : -1;
+    c.there |= sees >= 0;
+    const int tiles = sees < 0 ? 0 : a.count == nullptr ? rf_pages(sees) : rf_cache_attn::listed(a, c.it, r / kPage);
+    if (j == 0) n[0] = tiles; else n[1] = tiles;
   }
-  return s;
+  c.n0 = n[0];
+  c.n1 = n[1];
+  return c;
 }
 struct ChunkPlaces {
   static constexpr int kRowsOf = kRows, kEnd = kItemPlaces;
-  static __device__ __noinline__ int of(const RfCacheAttn& a, int item) {
-    const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
-    if (it.sees < 0) return 0;
-    const Streams s = streams(a, it);
-    return max(s.n0, s.n1) + kItemPlaces;
+  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
+    const ChunkItem c = chunk_item(a, item);
+    return c.there ? max(c.n0, c.n1) + kItemPlaces : 0;
   }
 };
 
@@ -255,12 +255,13 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     RF_REGS_WIDEN();
     // ------------------------------------------------------------ Q in two parts, V's codes to bf16
     const int w = warp - kWidenWarp;
-    // An item's 256 rows, kLanes neighbouring lanes a row (16 bytes each), in place: a warp has read its rows before it writes their parts.
-    auto split_q = [&](int slot) {
+    // An item's rows, kLanes neighbouring lanes a row (16 bytes each), in place: a warp has read its rows before it writes their parts.  (What
+    // the parts of rows past the last hold does not matter: no such row is stored.)
+    auto split_q = [&](int slot, int rows) {
       constexpr int kLanes = D == 64 ? 8 : 16, kRowsAtOnce = 32 / kLanes, kTogether = 2;
       const int c = lane % kLanes;
 #pragma unroll 1
-      for (int s0 = w * kRowsAtOnce + lane / kLanes; s0 < kRows; s0 += 4 * kRowsAtOnce * kTogether) {
+      for (int s0 = w * kRowsAtOnce + lane / kLanes; s0 - lane / kLanes < rows; s0 += 4 * kRowsAtOnce * kTogether) {
         uint4 v[kTogether];
         uint32_t most[kTogether];             // the rows' largest magnitudes, as bf16 bits
 #pragma unroll
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       if (f & kFirst) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar(C::B_QR), nq & 1, wc))) break;
         ++nq;
-        split_q((int)r[3]);
+        split_q((int)r[3], min(kRows, a.u.rows - items[(int)r[3] * kItemWords + 1]));
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::B_Q));
@@ -355,9 +356,9 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       bool ok = true;
 #pragma unroll 1
       for (long long pos = st.lo; pos < st.hi && ok; ++item) {
-        const CacheItem it = rf_cache_attn::cache_item<kRows>(a, item);
-        if (it.sees < 0) continue;
-        const Streams s = streams(a, it);
+        const ChunkItem s = chunk_item(a, item);
+        const CacheItem it = s.it;
+        if (!s.there) continue;
         const int n = max(s.n0, s.n1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
         at += n + kItemPlaces;
         pos = min(at, st.hi);
@@ -860,14 +861,14 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   float m = -INFINITY, l = 0.f, lx = 0.f;
   int ref = -128;
   float4 acc[4] = {};
-#pragma unroll 1
+#pragma unroll 2
   for (int i = 0; i <= n; ++i) {
     const float4* at = pieces + ((i == 0 ? (size_t)2 * (x - 1) + 1 : (size_t)2 * (x + i - 1)) * 2 + j) * C::PIECE;
     const float4 st = __ldcg(at + (D / 4) * BM);
-    if (st.w == 0.f) continue;                          // walked no tile: its O was never written
     float4 o[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = __ldcg(at + (c0 + k) * BM);
+    if (st.w == 0.f) continue;                          // walked no tile: its O was never written
     float keep = 1.f, w = 1.f;
     if (st.x > m) {
       if (m > -INFINITY) keep = ex2(m - st.x);
