@@ -258,48 +258,53 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     // An item's rows, kLanes neighbouring lanes a row (16 bytes each), in place: a warp has read its rows before it writes their parts.  (What
     // the parts of rows past the last hold does not matter: no such row is stored.)
     auto split_q = [&](int slot, int rows) {
-      constexpr int kLanes = D == 64 ? 8 : 16, kRowsAtOnce = 32 / kLanes, kTogether = 2;
+      // Four steps' rows together, as a step is a chain of shuffles and conversions (9050 cycles for 256 rows two at a time and by way of
+      // fp32, 5120 so); rows' maxima in pairs.  In fp16 a scaled row and what hi leaves of it are exact down to 2^-24.
+      constexpr int kLanes = D == 64 ? 8 : 16, kRowsAtOnce = 32 / kLanes, kTogether = 4;
       const int c = lane % kLanes;
 #pragma unroll 1
       for (int s0 = w * kRowsAtOnce + lane / kLanes; s0 - lane / kLanes < rows; s0 += 4 * kRowsAtOnce * kTogether) {
         uint4 v[kTogether];
-        uint32_t most[kTogether];             // the rows' largest magnitudes, as bf16 bits
+        uint32_t most[kTogether / 2];         // two rows' largest magnitudes, as bf16 bits
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
           const int j = (s0 + k * 4 * kRowsAtOnce) >> 7, row = (s0 + k * 4 * kRowsAtOnce) & 127;
           const uint32_t at = D == 64 ? C::RAW + j * 128 * 128 : C::Q + (2 * j + (c >> 3)) * C::TILE;
           v[k] = c < D / 8 ? *reinterpret_cast<const uint4*>(base_ptr + at + row * 128 + (((c & 7) ^ (row & 7)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t* u = &v[k].x;
-          most[k] = 0u;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) most[k] = max(most[k], max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+          const uint32_t m = __vmaxu2(__vmaxu2(v[k].x & 0x7fff7fffu, v[k].y & 0x7fff7fffu), __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu));
+          const uint32_t one = max(m >> 16, m & 0xffffu);
+          most[k / 2] = k & 1 ? most[k / 2] | one << 16 : one;
         }
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) {
 #pragma unroll
-          for (int k = 0; k < kTogether; ++k) most[k] = max(most[k], __shfl_xor_sync(0xffffffffu, most[k], d));
+          for (int k = 0; k < kTogether / 2; ++k) most[k] = __vmaxu2(most[k], __shfl_xor_sync(0xffffffffu, most[k], d));
         }
         __syncwarp();
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
           const int rr = s0 + k * 4 * kRowsAtOnce, row = rr & 127;
           const uint32_t* u = &v[k].x;
+          const uint32_t top = k & 1 ? most[k / 2] >> 16 : most[k / 2] & 0xffffu;
           // times 2^e the largest lies in (224, 448]; a row with a value that is not finite gets that in its scale, so that its scores have it
-          const int e = most[k] == 0u ? 0 : min(8 - ((int)(most[k] >> 7) - 127) - ((most[k] & 127u) > 96u ? 1 : 0), 126);
+          const int e = top == 0u ? 0 : min(8 - ((int)(top >> 7) - 127) - ((top & 127u) > 96u ? 1 : 0), 126);
           const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-          if (c == 0) base_ptr[C::ROWEXP + slot * kRows + rr] = most[k] >= 0x7f80u ? 255 : (uint8_t)(127 - e);
-          uint32_t h2[4], l2[4];
+          if (c == 0) base_ptr[C::ROWEXP + slot * kRows + rr] = top >= 0x7f80u ? 255 : (uint8_t)(127 - e);
+          uint32_t hi[2] = {}, lo[2] = {};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float f0 = __uint_as_float(u[i] << 16) * up, f1 = __uint_as_float(u[i] & 0xffff0000u) * up;
-            h2[i] = __nv_cvt_float2_to_fp8x2(make_float2(f0, f1), __NV_SATFINITE, __NV_E4M3);
-            const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2[i], __NV_E4M3)));
-            l2[i] = __nv_cvt_float2_to_fp8x2(make_float2(f0 - back.x, f1 - back.y), __NV_SATFINITE, __NV_E5M2);
+            const uint32_t q2 = pack_f16(__uint_as_float(u[i] << 16) * up, __uint_as_float(u[i] & 0xffff0000u) * up);
+            const __half2_raw q2h = *reinterpret_cast<const __half2_raw*>(&q2);
+            const uint32_t h2 = __nv_cvt_halfraw2_to_fp8x2(q2h, __NV_SATFINITE, __NV_E4M3);
+            const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&q2), __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3)));
+            const uint32_t l2 = __nv_cvt_halfraw2_to_fp8x2(*reinterpret_cast<const __half2_raw*>(&rest), __NV_SATFINITE, __NV_E5M2);
+            hi[i / 2] |= h2 << (16 * (i & 1));
+            lo[i / 2] |= l2 << (16 * (i & 1));
           }
           if (c < D / 8) {
             const uint32_t at = base + C::Q + (rr >> 7) * 2 * C::TILE + C::qchunk(row, c >> 1) + (c & 1) * 8;
-            sts64(at, h2[0] | h2[1] << 16, h2[2] | h2[3] << 16);
-            sts64(at + C::TILE, l2[0] | l2[1] << 16, l2[2] | l2[3] << 16);
+            sts64(at, hi[0], hi[1]);
+            sts64(at + C::TILE, lo[0], lo[1]);
           }
         }
       }
