@@ -346,7 +346,7 @@ rf_status rf_arm_classify_noalloc(const rf_shape *shape, const rf_params *params
  * A page holds RF_CACHE_PAGE tokens of one sequence, all K/V heads; a sequence is a row of the page table: its token t lies in
  * page page_table[t / RF_CACHE_PAGE].  Stored values are e4m3 codes times a power of two, one per page, head and tensor (a block of
  * RF_CACHE_PAGE tokens): such a product is exactly a bf16 value, so the attention kernels round nothing when they widen it.
- * Codes 0x7f and 0xff (NaN) are never written and must not be: they are read as +-480.
+ * Codes 0x7f and 0xff (NaN) are never written.
  *
  * Everything below is device memory owned by the caller; the struct itself is host memory, read during the call.  A page is
  * free when no row names it among its first ceil(seq_len / RF_CACHE_PAGE) entries: there are no reference counts to keep, and
@@ -354,7 +354,8 @@ rf_status rf_arm_classify_noalloc(const rf_shape *shape, const rf_params *params
  * the table, is not read.  All pages may start uninitialised; a new cache has seq_len = 0 everywhere.
  *
  * Calls that write to a cache and calls that read it are ordered by the caller (one stream, or events), like any buffer's.
- * Limits: D in {64, 96, 128}; n_seqs <= 1024; heads * n_seqs <= 65535; n_pages <= 524288; max_pages <= 2^23.
+ * Limits: D in {64, 96, 128}; n_seqs <= 1024; heads * n_seqs <= 65535; n_pages <= 524288; n_pages * heads < 2^31; max_pages <= 2^23.
+ * The first call of each kind on a device sets kernel attributes: make it outside any stream capture.
  * seq_len outside 0..max_pages * RF_CACHE_PAGE or a page number outside 0..n_pages-1 is reported as RF_ERR_INVALID_ARG through
  * dev_status: calls that write then change nothing, calls that read give arbitrary results for that sequence.
  */
@@ -447,7 +448,8 @@ rf_status rf_cache_select(const rf_cache *cache, const rf_cache_query *query, co
  *   sched   NULL, or count / kv_tile as rf_cache_select writes them, or the caller's own (ascending, each page once; a page past
  *           the sequence is reported as RF_ERR_INVALID_ARG and skipped)
  *   o       device bf16 [n_seqs, H, M, D], 16-byte aligned;  lse  device float [n_seqs, H, M] or NULL (natural log)
- *           A row that sees no key gets zeros and -inf.
+ *           A row that sees no key gets zeros and -inf.  (Products: K as stored; q within 2^-21 of its row's largest element; weights in
+ *           fp16, those below 2^-31 of the largest as zeros; V as stored, in chunks to 2^-25 of the largest page scale before it.)
  *   ws      rf_cache_attn_workspace_bytes() of device memory, 256-byte aligned, overwritten; calls that may overlap need one each
  */
 size_t rf_cache_attn_workspace_bytes(const rf_cache *cache, const rf_cache_query *query);

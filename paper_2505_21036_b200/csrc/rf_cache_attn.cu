@@ -25,6 +25,16 @@ namespace {
 
 enum { kFirst = 1, kLast = 2, kNothing = 4, kHeadPiece = 8, kTailPiece = 16, kEnd = 32 };
 
+// An item and the key tiles that it walks; -1: all of its rows are padding.
+struct TokenItem { CacheItem it; int tiles; };
+template <int kRows>
+static __device__ __noinline__ TokenItem token_item(const RfCacheAttn& a, int item) {
+  TokenItem t;
+  t.it = cache_item<kRows>(a, item);
+  const int sees = rf_rows_see(a.u, t.it.len, t.it.q_len, t.it.r0, kRows);
+  t.tiles = sees < 0 ? -1 : a.count == nullptr ? rf_pages(sees) : listed(a, t.it, t.it.r0 / kPage);
+  return t;
+}
 template <int D, int NB>
 struct Cfg {
   static constexpr int ROWS = 8 * NB, GROUPS = NB == 1 ? 2 : 1, WARPS = 8 * GROUPS, THREADS = 32 * (WARPS + 1);
@@ -36,7 +46,7 @@ struct Cfg {
   static constexpr uint32_t BAR = SUMS + WARPS * ROWS * 16;
   static constexpr uint32_t REC = BAR + 8 * (2 * SLOTS + 2);
   static constexpr uint32_t MISC = REC + SLOTS * 32;
-  static constexpr uint32_t TOTAL = MISC + 16 + sizeof(StretchScratch);
+  static constexpr uint32_t TOTAL = MISC + 16 + sizeof(StretchScratch<TokenItem>);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
   static constexpr int PIECE = ROWS * (D + 4);                      // floats: O [ROWS][D], then {m, l, l exact, 0} per row
@@ -72,23 +82,12 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   return d;
 }
 
-// An item and the key tiles that it walks; -1: all of its rows are padding.
-struct TokenItem { CacheItem it; int tiles; };
-template <int kRows>
-static __device__ __noinline__ TokenItem token_item(const RfCacheAttn& a, int item) {
-  TokenItem t;
-  t.it = cache_item<kRows>(a, item);
-  const int sees = rf_rows_see(a.u, t.it.len, t.it.q_len, t.it.r0, kRows);
-  t.tiles = sees < 0 ? -1 : a.count == nullptr ? rf_pages(sees) : listed(a, t.it, t.it.r0 / kPage);
-  return t;
-}
 template <int kRows>
 struct TokenPlaces {
   static constexpr int kRowsOf = kRows, kEnd = 6;     // what an item costs beside its tiles: Q, the meeting of the warps, its outputs
-  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
-    const int n = token_item<kRows>(a, item).tiles;
-    return n < 0 ? 0 : n + kEnd;
-  }
+  using Info = TokenItem;
+  static __device__ __forceinline__ TokenItem look(const RfCacheAttn& a, int item) { return token_item<kRows>(a, item); }
+  static __device__ __forceinline__ int of(const TokenItem& t) { return t.tiles < 0 ? 0 : t.tiles + kEnd; }
 };
 
 struct Maps { CUtensorMap k, v; };
@@ -105,7 +104,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
   const uint32_t joined = base + C::BAR + 8u * (2 * C::SLOTS), read = joined + 8;   // all warps' rows of an item are in shared memory; they have been read
   volatile Record* records = reinterpret_cast<volatile Record*>(base_ptr + C::REC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC);
-  StretchScratch* scratch = reinterpret_cast<StretchScratch*>(base_ptr + C::MISC + 16);
+  StretchScratch<TokenItem>* scratch = reinterpret_cast<StretchScratch<TokenItem>*>(base_ptr + C::MISC + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
 #pragma unroll 1
@@ -146,7 +145,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     };
 #pragma unroll 1
     for (long long pos = st.lo; pos < st.hi; ++item) {
-      const TokenItem ti = token_item<kRows>(a, item);
+      const TokenItem ti = item == st.item ? scratch->info : token_item<kRows>(a, item);
       const CacheItem it = ti.it;
       const int tiles = ti.tiles;
       if (tiles < 0) continue;
@@ -405,6 +404,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
         } else if (place < it.q_len) {
           const float inv = ll == 0.f ? 0.f : 1.f / ll;            // (a sum that is no number stays one)
           const size_t at_row = (size_t)it.bh * a.u.rows + it.r0 + r;
+          if (!rf_in_bounds(at_row, (unsigned long long)a.c.B * a.c.H * a.u.rows, a.dev_status)) continue;
           *reinterpret_cast<uint2*>(a.o + at_row * D + d4 * 4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
           if (LSE && d4 == 0) a.lse[at_row] = (mm + log2f(llx)) * 0.6931471805599453f;
         }
@@ -466,6 +466,7 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const size_t at_row = (size_t)it.bh * a.u.rows + row;
+  if (!rf_in_bounds(at_row, (unsigned long long)a.c.B * a.c.H * a.u.rows, a.dev_status)) return;
   a.o[at_row * D + tid] = __float2bfloat16_rn(acc * inv);
   if (LSE && tid == 0) a.lse[at_row] = (mm + log2f(lx)) * 0.6931471805599453f;
 }

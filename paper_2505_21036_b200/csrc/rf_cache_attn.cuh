@@ -48,18 +48,23 @@ __device__ __forceinline__ int listed(const RfCacheAttn& a, const CacheItem& it,
 // some that stand for what an item costs beside them, at least one, so that a row block that sees nothing has its outputs written).
 // cuts: lo lies among that item's tiles, behind the first.
 struct Stretch { long long lo, hi, at; int item, cuts; };
-struct StretchScratch { long long sums[33]; Stretch st; };
+template <typename Info>
+struct StretchScratch { long long sums[33]; Stretch st; Info info; };    // info: that item, looked up
 
-// Called by all threads of the CTA (kThreads of them, whole warps).  Places::of(a, item): the item's places on the line, kEnd of
-// them at its end for itself; 0 for an item whose rows are all padding.
+// Called by all threads of the CTA (kThreads of them, whole warps).  Places::look(a, item): the item; Places::of(info): its places on the
+// line, kEnd of them at its end for itself; 0 for an item whose rows are all padding.
 template <typename Places, int kThreads>
-__device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch* s) {
+__device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch<typename Places::Info>* s) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int items = a.c.B * a.c.H * rf_cdiv(a.u.rows, Places::kRowsOf), per = rf_cdiv(items, kThreads);
   const int i0 = min(tid * per, items), i1 = min(i0 + per, items);
   long long mine = 0;
+  typename Places::Info info = {};
 #pragma unroll 1
-  for (int i = i0; i < i1; ++i) mine += Places::of(a, i);
+  for (int i = i0; i < i1; ++i) {
+    info = Places::look(a, i);
+    mine += Places::of(info);
+  }
   long long x = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -83,9 +88,11 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch*
     int i = i0;
 #pragma unroll 1
     for (;; ++i) {
-      const int p = Places::of(a, i);
+      if (per > 1) info = Places::look(a, i);              // (a thread's only item is at hand)
+      const int p = Places::of(info);
       if (lo < at + p) {
         s->st = Stretch{lo, hi, at, i, at < lo && lo < at + p - Places::kEnd};
+        s->info = info;
         break;
       }
       at += p;

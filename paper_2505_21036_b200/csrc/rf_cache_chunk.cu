@@ -65,6 +65,34 @@ constexpr float kTop = 7.0f, kRaise = 8.0f, kRaiseMargin = 3.0f;
 constexpr int kMostUp = 7;                                  // a page's V scale above the reference, in log2
 constexpr int kSpec = 32;
 
+// What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
+constexpr int kItemPlaces = 6;
+
+// An item and the two streams' lists: how long they are.  there: some row is no padding.
+struct ChunkItem { CacheItem it; int n0, n1; bool there; };
+static __device__ __noinline__ ChunkItem chunk_item(const RfCacheAttn& a, int item) {
+  ChunkItem c;
+  c.it = rf_cache_attn::cache_item<kRows>(a, item);
+  int n[2];
+  c.there = false;
+#pragma unroll 1
+  for (int j = 0; j < 2; ++j) {
+    const int r = c.it.r0 + j * BM, sees = r < a.u.rows ? rf_rows_see(a.u, c.it.len, c.it.q_len, r, BM) : -1;
+    c.there |= sees >= 0;
+    const int tiles = sees < 0 ? 0 : a.count == nullptr ? rf_pages(sees) : rf_cache_attn::listed(a, c.it, r / kPage);
+    if (j == 0) n[0] = tiles; else n[1] = tiles;
+  }
+  c.n0 = n[0];
+  c.n1 = n[1];
+  return c;
+}
+struct ChunkPlaces {
+  static constexpr int kRowsOf = kRows, kEnd = kItemPlaces;
+  using Info = ChunkItem;
+  static __device__ __forceinline__ ChunkItem look(const RfCacheAttn& a, int item) { return chunk_item(a, item); }
+  static __device__ __forceinline__ int of(const ChunkItem& c) { return c.there ? max(c.n0, c.n1) + kItemPlaces : 0; }
+};
+
 // TMEM columns and V's layout are those of the clip kernel (rf_attn.cu: Cfg), where they are explained: V in blocks of VBOX columns with a block of ones behind them whose product is
 // the row sum of the rounded weights, P on top of S (D = 96 / 128) or in columns of its own (D = 64).
 template <int D>
@@ -96,7 +124,7 @@ struct Cfg {
   static constexpr uint32_t ROWEXP = WINDOW + 4 * kBatch * 4;               // by item slot: exponent field of what undoes a row's scaling
   static_assert(ROWEXP % 8 == 0 && (ROWEXP + kItemSlots * kRows) % 8 == 0, "alignment");
   static constexpr uint32_t SCRATCH = ROWEXP + kItemSlots * kRows;
-  static constexpr uint32_t TOTAL = SCRATCH + sizeof(StretchScratch);
+  static constexpr uint32_t TOTAL = SCRATCH + sizeof(StretchScratch<ChunkItem>);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
   static constexpr bool S_SHARED = D != 96;
@@ -105,35 +133,6 @@ struct Cfg {
   static constexpr uint32_t O_COL0 = S_EARLY ? S_END + 128 : S_END, O_COL1 = O_COL0 + NPV;
   static_assert(O_COL1 + NPV <= TMEM_COLS, "TMEM columns");
   static constexpr size_t PIECE = (size_t)(D / 4 + 1) * BM;                 // float4 of one piece of one stream: O, then {m, l, l exact, 128 + V's reference or 0: no O}
-};
-
-// What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
-constexpr int kItemPlaces = 6;
-
-// An item and the two streams' lists: how long they are.  there: some row is no padding.
-struct ChunkItem { CacheItem it; int n0, n1; bool there; };
-static __device__ __noinline__ ChunkItem chunk_item(const RfCacheAttn& a, int item) {
-  ChunkItem c;
-  c.it = rf_cache_attn::cache_item<kRows>(a, item);
-  int n[2];
-  c.there = false;
-#pragma unroll 1
-  for (int j = 0; j < 2; ++j) {
-    const int r = c.it.r0 + j * BM, sees = r < a.u.rows ? rf_rows_see(a.u, c.it.len, c.it.q_len, r, BM) : -1;
-    c.there |= sees >= 0;
-    const int tiles = sees < 0 ? 0 : a.count == nullptr ? rf_pages(sees) : rf_cache_attn::listed(a, c.it, r / kPage);
-    if (j == 0) n[0] = tiles; else n[1] = tiles;
-  }
-  c.n0 = n[0];
-  c.n1 = n[1];
-  return c;
-}
-struct ChunkPlaces {
-  static constexpr int kRowsOf = kRows, kEnd = kItemPlaces;
-  static __device__ __forceinline__ int of(const RfCacheAttn& a, int item) {
-    const ChunkItem c = chunk_item(a, item);
-    return c.there ? max(c.n0, c.n1) + kItemPlaces : 0;
-  }
 };
 
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
@@ -203,6 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   volatile int* abort_flag = reinterpret_cast<volatile int*>(base_ptr + C::MISC + 8);
   int* items = reinterpret_cast<int*>(base_ptr + C::ITEM);
   volatile uint32_t* records = reinterpret_cast<volatile uint32_t*>(base_ptr + C::RECORD);
+  StretchScratch<ChunkItem>* scratch = reinterpret_cast<StretchScratch<ChunkItem>*>(base_ptr + C::SCRATCH);
   volatile int* refs = reinterpret_cast<volatile int*>(base_ptr + C::REF);
   volatile uint32_t* flags = reinterpret_cast<volatile uint32_t*>(base_ptr + C::FLAGS);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
   }
   rf_grid_wait();
   tc_fence_before();
-  const Stretch st = rf_cache_attn::stretch<ChunkPlaces, kThreads>(a, reinterpret_cast<StretchScratch*>(base_ptr + C::SCRATCH));   // (has barriers)
+  const Stretch st = rf_cache_attn::stretch<ChunkPlaces, kThreads>(a, scratch);   // (has barriers)
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   const WaitCtx wc{abort_flag, a.dev_status};
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
 
   if (warp >= kWidenWarp) {
     RF_REGS_WIDEN();
-    // ------------------------------------------------------------ Q in two parts, V's codes to bf16
+    // ------------------------------------------------------------ Q in two parts, V's codes to fp16
     const int w = warp - kWidenWarp;
     // An item's rows, kLanes neighbouring lanes a row (16 bytes each), in place: a warp has read its rows before it writes their parts.  (What
     // the parts of rows past the last hold does not matter: no such row is stored.)
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       bool ok = true;
 #pragma unroll 1
       for (long long pos = st.lo; pos < st.hi && ok; ++item) {
-        const ChunkItem s = chunk_item(a, item);
+        const ChunkItem s = item == st.item ? scratch->info : chunk_item(a, item);
         const CacheItem it = s.it;
         if (!s.there) continue;
         const int n = max(s.n0, s.n1), begin = (int)(pos - at), end = (int)min((long long)n, st.hi - at);
@@ -808,8 +808,8 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         }
         __stcg(mine + (D / 4) * BM, make_float4(m_run, l_run, l_exact, n > 0 ? (float)(ref_run + 128) : 0.f));
       } else {
-        const bool there = r < a.u.rows && r % a.u.M < iw[3];
         const size_t at_row = (size_t)iw[0] * a.u.rows + min(r, a.u.rows - 1);
+        const bool there = r < a.u.rows && r % a.u.M < iw[3] && rf_in_bounds(at_row, (unsigned long long)a.c.B * a.c.H * a.u.rows, a.dev_status);
         uint4* o = reinterpret_cast<uint4*>(a.o + at_row * D);
         const bool o32 = (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0;
         const float inv = l_run == 0.f ? 0.f : pow2i(ref_run) / l_run;
@@ -903,6 +903,7 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
     v[2 * k + 1] = pack_bf16(acc[k].z * inv, acc[k].w * inv);
   }
   const size_t at_row = (size_t)it.bh * a.u.rows + row;
+  if (!rf_in_bounds(at_row, (unsigned long long)a.c.B * a.c.H * a.u.rows, a.dev_status)) return;
   store_sector(reinterpret_cast<uint4*>(a.o + at_row * D) + c0 / 2, v, (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0);
   if (LSE && c0 == 0) a.lse[at_row] = (m - kTop + log2f(lx)) * 0.6931471805599453f;
 }
