@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) rf_cache_select_kernel(RfCache
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[d][k] = g < T ? pooled[g < T ? g : 0][16 * d + 4 * q4 + k] : 0.0;
+      for (int k = 0; k < 4; ++k) w[d][k] = T == 1 || g < T ? pooled[T == 1 ? 0 : g % T][16 * d + 4 * q4 + k] : 0.0;
 #pragma unroll 1
     for (int c0 = keep_first + warp * 8; c0 < most; c0 += kSelWarps * 8) {
       const int col = c0 + g;
@@ -602,12 +602,26 @@ __global__ void __launch_bounds__(kSelThreads, 1) rf_cache_select_kernel(RfCache
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) v[d] = there ? x[4 * d] : make_float4(0.f, 0.f, 0.f, 0.f);
       double dot[2] = {};
+      if constexpr (T == 1) {                               // one column: as multiplications, the four lanes of a page add theirs up
+        double sum[4] = {};
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) {
-        mma_f64(dot, (double)v[d].x, w[d][0]);
-        mma_f64(dot, (double)v[d].y, w[d][1]);
-        mma_f64(dot, (double)v[d].z, w[d][2]);
-        mma_f64(dot, (double)v[d].w, w[d][3]);
+        for (int d = 0; d < D / 16; ++d) {
+          sum[0] += (double)v[d].x * w[d][0];
+          sum[1] += (double)v[d].y * w[d][1];
+          sum[2] += (double)v[d].z * w[d][2];
+          sum[3] += (double)v[d].w * w[d][3];
+        }
+        dot[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 1);
+        dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], 2);
+      } else {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          mma_f64(dot, (double)v[d].x, w[d][0]);
+          mma_f64(dot, (double)v[d].y, w[d][1]);
+          mma_f64(dot, (double)v[d].z, w[d][2]);
+          mma_f64(dot, (double)v[d].w, w[d][3]);
+        }
       }
       const double tokens = (double)min(kPage, len - col * kPage);
 #pragma unroll

@@ -56,7 +56,7 @@ struct Cfg {
   }
 };
 
-struct Record { int item, page, flags; float ks, vs; };
+struct Record { int item, page, flags, len, q_len; float ks, vs; };
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       const int n = sent[group], s = group * C::STAGES + n % C::STAGES;
       if (!wait_for(empty(s), ((n / C::STAGES) & 1) ^ 1, wc)) return;        // (the first round finds them free) abandoned: nothing more is fetched
       volatile Record* d = records + s;
-      d->item = r.item; d->page = r.page; d->flags = r.flags;
+      d->item = r.item; d->page = r.page; d->flags = r.flags; d->len = r.len; d->q_len = r.q_len;
       d->ks = r.ks; d->vs = r.vs;
       if (bytes) {
         const uint32_t to = base + s * 2 * C::TILE;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
 #pragma unroll 1
         for (int i = 0; i < batch; ++i) {
           Record s;
-          s.item = item;
+          s.item = item; s.len = it.len; s.q_len = it.q_len;
           s.page = __shfl_sync(0xffffffffu, r.page, i);
           s.flags = __shfl_sync(0xffffffffu, r.flags, i);
           s.ks = __shfl_sync(0xffffffffu, r.ks, i);
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     }
     if (lane == 0)
 #pragma unroll 1
-      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0.f, 0.f}, g, false, 0);
+      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0, 0, 0.f, 0.f}, g, false, 0);
   } else {
     // ------------------------------------------------------------ consumers: 16 keys of every tile of their group each
     const int g = lane >> 2, t = lane & 3, group = warp >> 3, slice = 16 * (warp & 7);
@@ -218,12 +218,15 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       Record rec;
       {
         volatile const Record* r = records + slot;
-        rec.item = r->item; rec.page = r->page; rec.flags = r->flags;
+        rec.item = r->item; rec.page = r->page; rec.flags = r->flags; rec.len = r->len; rec.q_len = r->q_len;
         rec.ks = r->ks; rec.vs = r->vs;
       }
       if (rec.flags & kEnd) break;
       if (rec.flags & kFirst) {
-        it = token_item<kRows>(a, rec.item).it;
+        it.bh = rec.item;                                          // (all rows of a K/V head are one item here)
+        it.r0 = 0;
+        it.len = rec.len;
+        it.q_len = rec.q_len;
         const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
         int row_sees = -1;                                         // keys that row `lane` sees; -1: it is not there
         if (lane < kRows && it.r0 + lane < a.u.rows) {
