@@ -190,6 +190,18 @@ def test_scales_past_the_exponent_that_one_product_reaches(M):
     p2.attend(rng.standard_normal((1, 2, M, 64)) * 2.0 ** -14)
 
 
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("M,causal", [(1, 0), (640, 128), (640, 1), (300, 0)])
+def test_values_whose_scale_varies_from_page_to_page(D, M, causal):
+    """V's pages 2^-14 to 2^16 apart: units that change under rows that see some of them only.  (Within 2^15 below the largest, where V is
+    exact in any unit.)"""
+    p = Pair(1, 2, D, 10, 10)
+    rng = np.random.default_rng(D + M)
+    for e in (0, 9, -5, 12, 1):
+        p.append(rng.standard_normal((1, 2, 128, D)), rng.standard_normal((1, 2, 128, D)) * 2.0 ** e, [128])
+    p.attend(rng.standard_normal((1, 4, M, D)) * 3, causal=causal)
+
+
 @pytest.mark.parametrize("M", [1, 130])
 def test_a_query_that_is_no_number_spoils_its_own_row_only(M):
     p, rng = filled(1, 1, 64, [300])
