@@ -89,9 +89,10 @@ __device__ __forceinline__ bool mark_pages(const RfCache& c, const int* lens, ui
 // ------------------------------------------------------------------------------------------------ append
 // Pages for the tokens that come, and the sequences' new lengths.  One CTA: what it does is a chain of a dozen round trips
 // to the L2, 5 to 7 us, whatever the pool's size up to some ten thousand pages.
+constexpr int kFew = 1024;
 __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, int M, const int32_t* new_len, int32_t* ws, int32_t* dev_status) {
   extern __shared__ uint32_t bits[];
-  __shared__ int scan[33], lens[kCacheMaxSeqs], need_at[kCacheMaxSeqs + 1], most;
+  __shared__ int scan[33], lens[kCacheMaxSeqs], need_at[kCacheMaxSeqs + 1], most, few[kFew];
   const int tid = threadIdx.x, words = (c.n_pages + 31) / 32;
   uint32_t *used = bits, *twice = bits + words;
   const PlanWs w = plan_ws(ws, c.B, c.n_pages);
@@ -108,15 +109,17 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
     full = !bad && (long long)len + add > min(most, 0x7fffffffll);
     lens[tid] = bad ? 0 : len;
   }
+  // the sequence's partly filled last page (looked at once the table is known to be in order)
+  int old_page = -1;
+  if (tid < c.B && !bad && !full && add > 0 && len % kPage != 0) old_page = c.table[(size_t)tid * c.max_pages + len / kPage];
   bad = __syncthreads_or(bad);
   if (!bad) bad = !mark_pages(c, lens, used, twice, words, &most);
   // fresh pages of this thread's sequence; its partly filled last page is among them if others name it too
-  int need = 0, first_new = 0, shared_page = 0, old_page = -1;
+  int need = 0, first_new = 0, shared_page = 0;
   if (!bad && tid < c.B && add > 0 && !full) {
     first_new = rf_pages(len);
     need = rf_pages(len + add) - first_new;
     if (len % kPage != 0) {
-      old_page = c.table[(size_t)tid * c.max_pages + len / kPage];
       shared_page = (twice[old_page >> 5] >> (old_page & 31)) & 1u;
       need += shared_page;
     }
@@ -137,12 +140,13 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
     if (tid < c.B) w.n_new[tid] = 0;
     return;
   }
+  int32_t* list = total <= kFew ? few : w.list;              // fresh pages in the order they are handed out
   if (tid < c.B) need_at[tid] = at;
   if (tid == 0) need_at[c.B] = total;
 #pragma unroll 1
   for (int i = w0; i < w1 && rank < total; ++i)
 #pragma unroll 1
-    for (uint32_t f = free_of(i); f != 0u && rank < total; f &= f - 1u) w.list[rank++] = i * 32 + __ffs(f) - 1;
+    for (uint32_t f = free_of(i); f != 0u && rank < total; f &= f - 1u) list[rank++] = i * 32 + __ffs(f) - 1;
   if (tid < c.B) {
     w.old_len[tid] = len;
     w.n_new[tid] = add;
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, 
       if (need_at[mid] <= i) lo = mid; else hi = mid - 1;
     }
     const int col = lens[lo] + i - need_at[lo];
-    if (rf_in_bounds(col, c.max_pages, dev_status)) c.table[(size_t)lo * c.max_pages + col] = w.list[i];
+    if (rf_in_bounds(col, c.max_pages, dev_status)) c.table[(size_t)lo * c.max_pages + col] = list[i];
   }
 }
 
@@ -231,8 +235,9 @@ __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const 
   for (int p = 0; p < kPasses; ++p) {
     const uint32_t* u = &v[p].x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) most = max(most, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+    for (int i = 0; i < 4; ++i) most = __vmaxu2(most, u[i] & 0x7fff7fffu);
   }
+  most = max(most >> 16, most & 0xffffu);
   if (most >= 0x7f80u) {                                     // something is not finite: NaN becomes zero, infinities saturate
     rf_report(dev_status, RF_ERR_NOT_FINITE);
     most = 0u;
