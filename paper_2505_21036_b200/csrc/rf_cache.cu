@@ -88,7 +88,7 @@ __device__ __forceinline__ bool mark_pages(const RfCache& c, const int* lens, ui
 
 // ------------------------------------------------------------------------------------------------ append
 // Pages for the tokens that come, and the sequences' new lengths.  One CTA: what it does is a chain of a dozen round trips
-// to the L2, 5 to 7 us, whatever the pool's size up to some ten thousand pages.
+// to the L2, about 5 us, whatever the pool's size up to some ten thousand pages.
 constexpr int kFew = 1024;
 __global__ void __launch_bounds__(kPlanThreads) rf_cache_plan_kernel(RfCache c, int M, const int32_t* new_len, int32_t* ws, int32_t* dev_status) {
   extern __shared__ uint32_t bits[];
@@ -493,7 +493,8 @@ __global__ void __launch_bounds__(256) rf_cache_move_kernel(RfCache c, const int
 // exact arithmetic hardly ever agree to 1e-16.  What bounds it: widening the key sums to 64 bits (16 a cycle and SM) and the 64-bit
 // products, so the tiles are the columns and the pages the rows of a 64-bit matrix product: a lane widens a number once for eight tiles and
 // holds its part of the tiles' sums in registers.  (29 tiles x 931 pages x 24 heads: 136 us with a tile a CTA, 67 with a lane a page and
-// four tiles a CTA, whose loads touched 32 rows at a time.)
+// four tiles a CTA, whose loads touched 32 rows at a time, 40 so.  A single tile, which would waste seven of the eight columns, is multiplied
+// without matrix products: a token each of 32 heads 21 and 16 us.)
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 
 __device__ __forceinline__ uint64_t ordered(double x) {   // monotone; NaN below everything

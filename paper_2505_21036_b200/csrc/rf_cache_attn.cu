@@ -6,7 +6,7 @@
 // take 16 keys of a tile each, on mma.sync with the keys as its 16 rows and the queries as its 8 columns (tcgen05 would spend 128 rows on
 // them): S^T = K q^T, then O^T += V^T P^T with P^T turned round by movmatrix.  Codes are widened to fp16 in registers, exactly, by one
 // conversion a pair (to bf16 it takes seven integer instructions and two products for four, and the integer pipe was what bound it: 152 us
-// for 33 frames of 3600 tokens, 24 heads).  So the other operands are fp16 too: a query row scaled by a power of two to a largest
+// for 33 frames of 3600 tokens, 24 heads; 129 so, 5.7 TB/s).  So the other operands are fp16 too: a query row scaled by a power of two to a largest
 // magnitude in [2^14, 2^15) (exact down to 2^-29 of that, 2^-40 of it beyond), and the weights times 2^15, whose largest is exact here
 // (11 bits, to 2^-39 of the largest).  The scales of rows and pages are applied in fp32.  The order
 // of a contraction is free, so the words are used as they lie: a word of K is four of the 16 terms of one instruction, and V's bytes
