@@ -7,7 +7,7 @@
 // Scores: K's codes go to the tensor cores as they are (kind::f8f6f4), and each query row, which is bf16, as a sum of two 8-bit
 // numbers.  With the row scaled by a power of two to a largest magnitude in (224, 448], hi = e4m3(q) leaves at most 8 units of q's last place, which
 // e5m2 holds exactly: q = hi + lo exactly from 2^-6 up (2^-14 of the row's largest), and below to within 2^-14 (2^-21.8 of the largest, the
-// order of an fp32 sum's own rounding).  hi K^T + lo K^T costs what one bf16 product costs, reads half the shared memory, and nothing has
+// order of an fp32 sum's own rounding).  hi K^T + lo K^T costs what one bf16 product costs, K takes half the shared memory, and nothing has
 // to be widened; the page's scale and the row's go into the softmax's factor.
 // Values: V is widened to fp16 by four warps (one conversion a pair of codes, exact), once for the 256 rows, and laid out in shared memory in
 // the swizzled form that tcgen05 reads, beside the softmax.  A page's scale has to go into V or into the weights, as O adds up over pages:
@@ -16,8 +16,8 @@
 // which 2^24 below still is bf16's precision).  The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to
 // 2^-21 of the maximum and to 2^-31 of it in steps; a row of a million keys loses 2^-12 of its weight at most.
 // (V to bf16 in seven integer instructions and two products for four codes: 2050 cycles of the widening warps' 3470 a tile, beside the softmax
-// on the same integer pipes; 24 heads, 2040 rows, 32 896 keys, D = 128: 784 us, with the widening left out 686.  K widened as well, by the
-// same four warps: 1090.)
+// on the same integer pipes; 24 heads, 2040 rows, 32 896 keys, D = 128: 784 us, to fp16 764 (1070 TFLOP/s), with the widening left out 686.  K
+// widened as well, by the same four warps: 1090.  Repeated for a second the board's power limits it: 867.)
 // Warp roles:
 //   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
 //   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q and the codes by TMA
