@@ -426,6 +426,7 @@ template <int D, int NB, bool LSE>
 __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant__ RfCacheAttn a, int ctas) {
   constexpr int kRows = 8 * NB, PIECE = Cfg<D, NB>::PIECE;
   __shared__ float red[2][D / 32];
+  __shared__ int last;
   extern __shared__ float weight[];              // [ctas]
   rf_grid_wait();
   const int x = blockIdx.x + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y;
@@ -435,9 +436,7 @@ __global__ void __launch_bounds__(D) rf_cache_join_kernel(const __grid_constant_
   // the item begins in the stretch before, unless that one begins inside it too
   const int32_t* prev = mine - kHeadWords;
   if (prev[3] && prev[0] == mine[0]) return;
-  int n = 1;                                     // stretches x .. x + n - 1 begin inside the item
-#pragma unroll 1
-  while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
+  const int n = cuts_from(heads, x, ctas, &last);
   const CacheItem it = cache_item<kRows>(a, mine[0]);
   const int row = it.r0 + r;
   if (row >= a.u.rows || row % a.u.M >= it.q_len) return;

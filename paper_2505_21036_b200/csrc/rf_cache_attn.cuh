@@ -109,6 +109,20 @@ __device__ __forceinline__ Stretch stretch(const RfCacheAttn& a, StretchScratch<
 // Workspace: a head per CTA {the item its stretch begins in, -, -, whether it begins inside it}, then two
 // pieces per CTA: that of the item its stretch begins inside, that of the item its stretch ends inside.
 constexpr int kHeadWords = 4;
+// Stretches x, x + 1, .. that begin inside the item that stretch x begins inside.  Called by all threads of the CTA; *s: shared memory.
+__device__ __forceinline__ int cuts_from(const int32_t* heads, int x, int ctas, int* s) {
+  if (threadIdx.x == 0) *s = ctas - x;
+  __syncthreads();
+  const int item = heads[x * kHeadWords];
+#pragma unroll 1
+  for (int i = x + 1 + threadIdx.x; i < ctas; i += blockDim.x)
+    if (!heads[i * kHeadWords + 3] || heads[i * kHeadWords] != item) {
+      atomicMin(s, i - x);
+      break;
+    }
+  __syncthreads();
+  return *s;
+}
 __host__ __device__ __forceinline__ size_t head_floats(int ctas) { return ((size_t)ctas * kHeadWords + 63) / 64 * 64; }
 
 // Bytes 0 and 1, bytes 2 and 3 of a word of codes as fp16 pairs.

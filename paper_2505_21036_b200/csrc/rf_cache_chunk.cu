@@ -856,9 +856,8 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
   const int32_t* mine = heads + x * kHeadWords;
   if (!mine[3]) return;
   if (mine[3 - kHeadWords] && mine[-kHeadWords] == mine[0]) return;
-  int n = 1;
-#pragma unroll 1
-  while (x + n < ctas && heads[(x + n) * kHeadWords + 3] && heads[(x + n) * kHeadWords] == mine[0]) ++n;
+  __shared__ int last;
+  const int n = rf_cache_attn::cuts_from(heads, x, ctas, &last);
   const CacheItem it = rf_cache_attn::cache_item<kRows>(a, mine[0]);
   const int row = it.r0 + j * BM + threadIdx.x;
   if (row >= a.u.rows || row % a.u.M >= it.q_len) return;

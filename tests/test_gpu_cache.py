@@ -190,6 +190,20 @@ def test_scales_past_the_exponent_that_one_product_reaches(M):
     p2.attend(rng.standard_normal((1, 2, M, 64)) * 2.0 ** -14)
 
 
+@pytest.mark.parametrize("M", [1, 9, 200])
+@pytest.mark.parametrize("large", [30.0, 3000.0])
+def test_queries_with_one_large_element(M, large):
+    """Where the keys have nothing, so that the scores come from the small ones."""
+    p = Pair(1, 1, 128, 5, 5)
+    rng = np.random.default_rng(12)
+    k = rng.standard_normal((1, 1, 500, 128))
+    k[..., 7] = 0.0
+    p.append(k, rng.standard_normal((1, 1, 500, 128)), [500])
+    q = rng.standard_normal((1, 1, M, 128))
+    q[..., 7] = large
+    p.attend(q)
+
+
 @pytest.mark.parametrize("D", [64, 96, 128])
 @pytest.mark.parametrize("M,causal", [(1, 0), (640, 128), (640, 1), (300, 0)])
 def test_values_whose_scale_varies_from_page_to_page(D, M, causal):
@@ -488,3 +502,62 @@ def test_the_binding_refuses():
         api.rf_cache_attn_fwd(c, torch.zeros((2, 3, 3, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 3, 3, 64), dtype=torch.bfloat16, device="cuda"))
     with pytest.raises(api.RainFusionError):
         api.rf_cache_drop(c, first=ints([0, 0]))
+
+
+def test_the_most_sequences_and_pages():
+    """1024 sequences, 524288 pages: every free page is handed out, then there are none, then half of them come back."""
+    B, P, C = 1024, 1 << 19, 512
+    c = api.KVCache.empty(B, 1, 64, P, C, "cuda")
+    g = torch.Generator("cuda").manual_seed(4)
+    perm = torch.randperm(P, generator=g, device="cuda").to(torch.int32)
+    c.page_table[:, :511] = perm[:B * 511].view(B, 511)
+    c.seq_len.fill_(511 * 128)
+    c.k_sum.copy_(torch.arange(P, device="cuda")[:, None, None].expand(P, 1, 64).float())      # a page's mark
+    status, live = ints([0]), ints([0])
+    x = torch.ones((B, 1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    api.rf_cache_append(c, x, x, None, status)
+    assert int(status.item()) == 0
+    assert torch.equal(c.page_table[:, 511], perm[B * 511:].sort().values) and bool((c.seq_len == 511 * 128 + 1).all())
+    before = c.page_table.clone()
+    y = torch.ones((B, 1, 128, 64), dtype=torch.bfloat16, device="cuda")
+    api.rf_cache_append(c, y, y, None, status)
+    assert int(status.item()) == 8 and torch.equal(c.page_table, before) and bool((c.seq_len == 511 * 128 + 1).all())
+    status.zero_()
+    first, count = ints([0] * B), ints([256] * B)
+    api.rf_cache_drop(c, first, count, None, status)
+    assert torch.equal(c.page_table[:, :256], before[:, 256:])
+    marks = c.k_sum[c.page_table[:, :256].long(), 0, 0].clone()
+    api.rf_cache_compact(c, live, status)
+    now = c.page_table[:, :256].long()
+    assert int(live.item()) == B * 256 and int(status.item()) == 0 and torch.equal(now.flatten().sort().values, torch.arange(B * 256, device="cuda"))
+    assert torch.equal(c.k_sum[now, 0, 0], marks)
+    stays = before[:, 256:].long() < B * 256
+    assert torch.equal(now[stays], before[:, 256:].long()[stays])
+
+
+@pytest.mark.parametrize("M", [1, 130])
+def test_two_calls_on_one_cache_at_once(M):
+    """Readers of one cache on two streams, a workspace each, one of them with a schedule."""
+    p, rng = filled(2, 2, 96, [2000, 900])
+    q = [bf16(rng.standard_normal((2, 4, M, 96))).cuda() for _ in range(2)]
+    sched = api.CacheSchedule.empty(p.dev, 4, M, 6)
+    api.rf_cache_select(p.dev, q[1], sched, keep_last=2, top_k=4)
+    want = [torch.empty_like(x) for x in q]
+    for x, o, s in zip(q, want, (None, sched)):
+        api.rf_cache_attn_fwd(p.dev, x, o, sched=s)
+    ws, streams = [api.alloc_cache_attn_workspace(p.dev, 4, M) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    got = [[torch.empty_like(x) for _ in range(12)] for x in q]
+    torch.cuda.synchronize()
+    for i in range(12):
+        for j in range(2):
+            with torch.cuda.stream(streams[j]):
+                api.rf_cache_attn_fwd(p.dev, q[j], got[j][i], sched=(None, sched)[j], ws=ws[j])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, w) for o, w in zip(got, want) for x in o)
+
+
+@pytest.mark.parametrize("H,heads", [(1, 1), (48, 48), (40, 5), (64, 1)])
+def test_head_layouts(H, heads):
+    for M in (1, 3, 129):
+        p, rng = filled(1, heads, 64, [400], seed=H + M)
+        p.attend(rng.standard_normal((1, H, M, 64)), causal=1)
