@@ -311,6 +311,8 @@ __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const 
 }
 
 // ------------------------------------------------------------------------------------------------ fork, drop
+__device__ __forceinline__ bool broken_len(const RfCache& c, int len) { return len < 0 || (long long)len > (long long)c.max_pages * kPage; }
+
 // Thirty-two columns of the table: the old rows are taken into shared memory and written back in their new places.
 __global__ void __launch_bounds__(256) rf_cache_fork_kernel(RfCache c, const int32_t* parent, int32_t* dev_status) {
   extern __shared__ int rows[];                       // [B][32], then the lengths in CTA 0
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(256) rf_cache_fork_kernel(RfCache c, const int
   rf_grid_wait();
   bool bad = false;
 #pragma unroll 1
-  for (int b = tid; b < c.B; b += 256) bad |= parent[b] < -1 || parent[b] >= c.B;
+  for (int b = tid; b < c.B; b += 256) bad |= parent[b] < -1 || parent[b] >= c.B || broken_len(c, c.len[b]);
 #pragma unroll 1
   for (int b = warp; b < c.B; b += 8)
     if (col < c.max_pages) rows[b * 32 + lane] = c.table[(size_t)b * c.max_pages + col];
@@ -350,14 +352,11 @@ __global__ void __launch_bounds__(256) rf_cache_drop_kernel(RfCache c, const int
   for (int i = tid; i < c.B; i += 256) {
     if (max_len != nullptr) bad |= max_len[i] < 0;
     if (first != nullptr) bad |= first[i] < 0 || count[i] < 0;
+    bad |= broken_len(c, c.len[i]);                    // (a length that another CTA has written already is in order before and after)
   }
   int len = c.len[b];                                  // (read by everybody before the barrier, written after it)
   if (__syncthreads_or(bad)) {
     if (b == 0 && tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
-    return;
-  }
-  if (len < 0 || (long long)len > (long long)c.max_pages * kPage) {
-    if (tid == 0) rf_report(dev_status, RF_ERR_INVALID_ARG);
     return;
   }
   if (max_len != nullptr) len = min(len, max_len[b]);

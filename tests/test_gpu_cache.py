@@ -127,6 +127,24 @@ def test_broken_arguments_are_reported_and_change_nothing():
         p.check("as before")
 
 
+@pytest.mark.parametrize("bad", [-1, 3 * 128 + 1])
+def test_a_broken_length_is_reported_and_changes_nothing(bad):
+    p, rng = filled(3, 1, 64, [130, 5, 260], M=100)
+    k, live = bf16(rng.standard_normal((3, 1, 50, 64))).cuda(), ints([0])
+    p.dev.seq_len[1] = bad
+    table = p.dev.page_table.clone()
+    for call in (lambda: api.rf_cache_append(p.dev, k, k, None, p.status), lambda: api.rf_cache_fork(p.dev, ints([2, 0, 1]), p.status),
+                 lambda: api.rf_cache_drop(p.dev, ints([0] * 3), ints([1] * 3), ints([9] * 3), p.status),
+                 lambda: api.rf_cache_compact(p.dev, live, p.status)):
+        call()
+        torch.cuda.synchronize()
+        assert int(p.status.item()) == 1 and torch.equal(p.dev.page_table, table) and p.dev.seq_len.tolist() == [130, bad, 260]
+        p.status.zero_()
+    assert int(live.item()) == -1
+    p.dev.seq_len[1] = 5
+    p.check("as before")
+
+
 def test_many_sequences_and_a_large_pool():
     rng = np.random.default_rng(5)
     p = Pair(700, 1, 64, 40000, 3)
