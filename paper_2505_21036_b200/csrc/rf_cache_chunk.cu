@@ -620,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
     const uint32_t t_s = tmem_base + lane_sel + (j ? C::S_COL1 : C::S_COL0);
     const uint32_t t_o = tmem_base + lane_sel + (j ? C::O_COL1 : C::O_COL0);
     const float sc = a.scale_log2;
-    uint32_t done = 0, nq = 0;
+    uint32_t done = 0;
     int waited = 0;
 #pragma unroll 1
     for (int item = 0;; ++item) {
@@ -651,9 +651,11 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         ks_next = k_scale[(size_t)place_of(page_next) * a.c.H];
         if (n > 1) place_next = place_of(page_of(begin + 1));
       }
-      if (waited > 0) {
-        mbar_wait(bar(C::B_Q), nq & 1, wc);
-        ++nq;
+      if (n > 0) {
+        // The rows' exponents are there once this stream's first scores are: the MMA thread has waited for Q before it issues them.  (B_Q itself
+        // must not be waited for here.  Nothing holds an item's Q back until these warps have seen the item's before it, so its one-bit parity could
+        // come round under a warp that is late.  The scores' barrier cannot: its next phase wants this warp's weights.)
+        mbar_wait(bar(C::B_SF + j), done & 1, wc);
         const uint32_t e = base_ptr[C::ROWEXP + slot * kRows + j * BM + row_in_tile];
         row_scale *= __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
       }
