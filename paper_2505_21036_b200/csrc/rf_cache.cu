@@ -739,11 +739,12 @@ __global__ void __launch_bounds__(kSelThreads, 1) rf_cache_select_kernel(RfCache
   if (rank == 0 && tile < u.n_q) count[row] = min(out, n_k);
 }
 
+// On a kernel's first use on a device, whatever this call's size: the 48 KB that need no asking are of static and dynamic memory together.
 template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes, bool (&done)[64]) {
+cudaError_t allow_smem(K kernel, bool (&done)[64]) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || bytes <= 48 * 1024 || (dev < 64 && done[dev])) return e;
+  if (e != cudaSuccess || (dev < 64 && done[dev])) return e;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024);
   if (e == cudaSuccess && dev < 64) done[dev] = true;
   return e;
@@ -757,7 +758,7 @@ cudaError_t rf_launch_cache_append(const RfCache& c, const __nv_bfloat16* k, con
                                    int32_t* ws, int32_t* dev_status, cudaStream_t st) {
   static bool done[64] = {};
   const size_t smem = 2 * sizeof(uint32_t) * rf_cdiv(c.n_pages, 32);
-  cudaError_t e = allow_smem(rf_cache_plan_kernel, smem, done);
+  cudaError_t e = allow_smem(rf_cache_plan_kernel, done);
   if (e != cudaSuccess) return e;
   e = rf_launch(rf_cache_plan_kernel, dim3(1), kPlanThreads, smem, st, c, M, new_len, ws, dev_status);
   if (e != cudaSuccess) return e;
@@ -772,7 +773,7 @@ cudaError_t rf_launch_cache_append(const RfCache& c, const __nv_bfloat16* k, con
 cudaError_t rf_launch_cache_fork(const RfCache& c, const int32_t* parent, int32_t* dev_status, cudaStream_t st) {
   static bool done[64] = {};
   const size_t smem = (size_t)c.B * 33 * sizeof(int);
-  cudaError_t e = allow_smem(rf_cache_fork_kernel, smem, done);
+  cudaError_t e = allow_smem(rf_cache_fork_kernel, done);
   if (e != cudaSuccess) return e;
   return rf_launch(rf_cache_fork_kernel, dim3(rf_cdiv(c.max_pages, 32)), 256, smem, st, c, parent, dev_status);
 }
@@ -785,7 +786,7 @@ cudaError_t rf_launch_cache_drop(const RfCache& c, const int32_t* first, const i
 cudaError_t rf_launch_cache_compact(const RfCache& c, int32_t* n_live, int32_t* ws, int32_t* dev_status, cudaStream_t st) {
   static bool done[64] = {};
   const size_t smem = sizeof(uint32_t) * rf_cdiv(c.n_pages, 32);
-  cudaError_t e = allow_smem(rf_cache_compact_plan_kernel, smem, done);
+  cudaError_t e = allow_smem(rf_cache_compact_plan_kernel, done);
   if (e != cudaSuccess) return e;
   e = rf_launch(rf_cache_compact_plan_kernel, dim3(1), kPlanThreads, smem, st, c, n_live, ws, dev_status);
   if (e != cudaSuccess) return e;
@@ -799,7 +800,7 @@ cudaError_t rf_launch_cache_select(const RfCache& c, const RfQueries& u, int kee
   const bool eight = u.n_q > 1 && 8 * sizeof(uint64_t) * (size_t)c.max_pages <= 128 * 1024;
   const size_t smem = (eight ? 8 : 1) * sizeof(uint64_t) * (size_t)c.max_pages;
   auto go = [&](auto kernel, bool (&done)[64]) -> cudaError_t {
-    const cudaError_t e = allow_smem(kernel, smem + 48 * 1024, done);   // (the static arrays count too)
+    const cudaError_t e = allow_smem(kernel, done);
     if (e != cudaSuccess) return e;
     return rf_launch(kernel, dim3(rf_cdiv(u.n_q, eight ? 8 : 1), c.H, c.B), kSelThreads, smem, st, c, u, keep_first, keep_last, top_k, count, pages, n_k, dev_status);
   };
