@@ -449,7 +449,8 @@ rf_status rf_cache_select(const rf_cache *cache, const rf_cache_query *query, co
  *           the sequence is reported as RF_ERR_INVALID_ARG and skipped)
  *   o       device bf16 [n_seqs, H, M, D], 16-byte aligned;  lse  device float [n_seqs, H, M] or NULL (natural log)
  *           A row that sees no key gets zeros and -inf.  (Products: K as stored; q within 2^-21 of its row's largest element; weights in
- *           fp16, those below 2^-31 of the largest as zeros; V as stored, in chunks to 2^-25 of the largest page scale before it.)
+ *           fp16, those below 2^-31 of the largest as zeros; V as stored.  In chunks (more than 16 rows a K/V head) V's error is up to 2^-76 of the
+ *           largest page scale that the tile, or a neighbour which lists the same page, has met on the way.)
  *   ws      rf_cache_attn_workspace_bytes() of device memory, 256-byte aligned, overwritten; calls that may overlap need one each
  */
 size_t rf_cache_attn_workspace_bytes(const rf_cache *cache, const rf_cache_query *query);

@@ -11,9 +11,9 @@
 // to be widened; the page's scale and the row's go into the softmax's factor.
 // Values: V is widened to fp16 by four warps (one conversion a pair of codes, exact), once for the 256 rows, and laid out in shared memory in
 // the swizzled form that tcgen05 reads, beside the softmax.  A page's scale has to go into V or into the weights, as O adds up over pages:
-// V is held in units of 2^ref, ref the scale of the piece's first page, in steps upwards where a page's scale is more than 2^7 above it (O
-// is then rescaled, as for a new maximum).  That is exact for scales down to 2^-15 of it; of smaller ones the last places go (2^-25 of 2^ref,
-// which 2^24 below still is bf16's precision).  The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to
+// V is held in units of 2^ref, ref the scale of the piece's first page, until a page's scale is more than 2^7 above it or 2^15 below, where fp16
+// would not hold it exactly: that page's scale is the next ref, and O is rescaled, as for a new maximum, in the rows that take
+// something of the page.  (Rare where a layer's pages are of like size.)  Only pages more than 2^60 below the largest unit so far lose places.  The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to
 // 2^-21 of the maximum and to 2^-31 of it in steps; a row of a million keys loses 2^-12 of its weight at most.
 // (V to bf16 in seven integer instructions and two products for four codes: 2050 cycles of the widening warps' 3470 a tile, beside the softmax
 // on the same integer pipes; 24 heads, 2040 rows, 32 896 keys, D = 128: 784 us, to fp16 764 (1070 TFLOP/s), with the widening left out 686.  K
@@ -62,7 +62,12 @@ static_assert(kRegsSoftmax == 200 && kRegsControl == 48 && kRegsWiden == 64, "ke
 // Lazy raising of the running maximum as in the clip kernel, but within what fp16 weights hold: a weight at the maximum is 2^kTop, one that
 // exceeds it by kRaise 2^15.
 constexpr float kTop = 7.0f, kRaise = 8.0f, kRaiseMargin = 3.0f;
-constexpr int kMostUp = 7;                                  // a page's V scale above the reference, in log2
+// V's reference scale, in log2: a page's scale is at most kMostUp above it (the largest code is then 57344) and at least -kLeastUp below it
+// (the least code 2^-24), where V is exact in fp16.  It goes up and down with the pages, but not more than kMostDown below where it has been for the rows,
+// whose O would not stay in fp32 otherwise: 2^30 keys of weight 2^15 and value 2^16 are below 2^61 of it.
+constexpr int kMostUp = 7, kLeastUp = -15, kMostDown = 60;
+constexpr float kNothing = 33.0f;                           // a score that far below the maximum has a weight of zero (2^kTop * 2^-32 is half of the least fp16 number):
+                                                            // a row that takes nothing of a tile keeps its unit, and its bits
 constexpr int kSpec = 32;
 
 // What an item costs beside its tiles (Q, the first scores, the last product, its outputs or pieces), in tiles.
@@ -144,7 +149,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 t = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
-__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+// 2^e for e <= 127, as far down as there are subnormal numbers.
+__device__ __forceinline__ float pow2i(int e) {
+  return __uint_as_float((uint32_t)(max(e < -126 ? e + 64 : e, -126) + 127) << 23) * (e < -126 ? 0x1p-64f : 1.f);
+}
 
 // Weights of the key columns [C0, C1) of a tile as in the clip kernel, packed to fp16.
 template <int C0, int C1, bool LSE>
@@ -388,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         ++no;
         if (e0 == b0 && e1 == b1) continue;                    // sees nothing, or lists nothing here
         bool first = true;
-        int ref = 0;
+        int ref = 0, top0 = -128, top1 = -128;                 // V's reference; the highest that it has been for either stream's rows
         const int32_t* l0 = a.count != nullptr ? a.pages + ((size_t)it.bh * a.u.n_q + it.r0 / kPage) * a.n_k : nullptr;
         const int32_t* l1 = l0 != nullptr && it.r0 / kPage + 1 < a.u.n_q ? l0 + a.n_k : l0;
         int i0 = b0, i1 = b1;
@@ -436,15 +444,18 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
             vexp = min(max((int)((__float_as_uint(a.c.v_scale[row]) >> 23) & 255u) - 127, -100), 100);
             valid = min(max(it.len - page * kPage, 0), kPage);
           }
-          // V's reference: the first tile's scale, raised where a tile's is too far above it
+          // V's reference: the first tile's scale, and another's where that is too far off
           int mine_ref = 0;
 #pragma unroll 1
           for (int i = 0; i < cnt; ++i) {
-            const int e = __shfl_sync(0xffffffffu, vexp, i);
-            if ((first && i == 0) || e > ref + kMostUp) ref = e;
+            const int e = __shfl_sync(0xffffffffu, vexp, i), on = (int)__shfl_sync(0xffffffffu, f, i);
+            const int least = max(on & 1 ? top0 : -128, on & 2 ? top1 : -128) - kMostDown;
+            if ((first && i == 0) || e > ref + kMostUp || e < ref + kLeastUp || ref < least) ref = max(e, least);
+            if (on & 1) top0 = max(top0, ref);
+            if (on & 2) top1 = max(top1, ref);
             if (lane == i) mine_ref = ref;
           }
-          const int up = vexp - mine_ref;                          // 2^up as fp16, subnormal or zero where it has to be
+          const int up = vexp - mine_ref;                          // 2^up as fp16; below 2^-15, or zero, at the least reference only
           const uint32_t half = up >= -14 ? (uint32_t)(up + 15) << 10 : up >= -24 ? 1u << (up + 24) : 0u;
           f |= (uint32_t)(mine_ref + 128) << 8;
           // the tiles one after the other, each by the lane that looked it up
@@ -673,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         const bool partial = __any_sync(0xffffffffu, left < BN);
         mbar_wait(bar(C::B_SF + j), done & 1, wc);
         tc_fence_after();
-        const int ref = refs[j];
+        const int tile_ref = refs[j];
         uint32_t s[128];
         uint32_t l_tile;
         if constexpr (!C::S_EARLY) l_tile = tmem_ld1(t_o + D);
@@ -698,6 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           }
           const float m_tile = fmaxf(mx0, mx1) * sc;
           const bool raise = m_tile > m_run + kRaise || (m_run == -INFINITY && m_tile > -INFINITY);
+          const int ref = opens || m_tile > m_run - kNothing ? tile_ref : ref_run;
           const bool any_raise = __any_sync(0xffffffffu, raise || ref != ref_run);
           float alpha = 1.f;
           if (raise) {
@@ -750,6 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
           mx1 = fmaxf(mx1, fmaxf(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])));
         }
         const float m_tile = fmaxf(mx0, mx1) * sc;
+        const int ref = opens || m_tile > m_run - kNothing ? tile_ref : ref_run;
         if (__any_sync(0xffffffffu, m_tile > m_run + kRaise || ref != ref_run)) {
           float alpha = 1.f;
           if (m_tile > m_run + kRaiseMargin) {
@@ -874,18 +887,19 @@ __global__ void __launch_bounds__(BM) rf_cache_chunk_join_kernel(const __grid_co
     float4 o[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = __ldcg(at + (c0 + k) * BM);
-    if (st.w == 0.f) continue;                          // walked no tile: its O was never written
+    if (st.w == 0.f || (st.x == -INFINITY && st.y == 0.f)) continue;   // walked no tile, so its O was never written, or saw nothing in them
     float keep = 1.f, w = 1.f;
     if (st.x > m) {
-      if (m > -INFINITY) keep = ex2(m - st.x);
+      keep = ex2(m - st.x);                             // (0 from -inf on)
       m = st.x;
     } else if (st.x > -INFINITY) {
       w = ex2(st.x - m);
     }
     l = l * keep + st.y * w;
     lx = lx * keep + st.z * w;
-    const int mine_ref = (int)st.w - 128, top = max(ref, mine_ref);
-    keep *= pow2i(ref - top);
+    if (w == 0.f) continue;                             // units count where there is something in them
+    const int mine_ref = (int)st.w - 128, top = keep == 0.f ? mine_ref : max(ref, mine_ref);
+    keep *= pow2i(min(ref - top, 0));
     w *= pow2i(mine_ref - top);
     ref = top;
 #pragma unroll
