@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       for (int t = begin; t < end; ++t, ++done, opens = false) {
         const int left = sees - page_next * kPage;        // keys of the tile that this row sees (page <= 2^23: no overflow)
         float sc = row_scale * ks_next;
-        if (sc < 1.1754944e-38f) sc = 1.1754944e-38f;     // (a masked score, -inf, times zero would be no number)
+        if (left <= 0 || sc < 1.1754944e-38f) sc = 1.1754944e-38f;   // (a masked score, -inf, times zero or NaN would be no number)
         if (t + 1 < end) {
           page_next = page_of(t + 1);
           ks_next = k_scale[(size_t)place_next * a.c.H];
