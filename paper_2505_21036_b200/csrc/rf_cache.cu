@@ -209,8 +209,9 @@ __global__ void __launch_bounds__(2 * D) rf_cache_write_kernel(RfCache c, const 
   const PlanWs w = plan_ws(const_cast<int32_t*>(ws), c.B, c.n_pages);
   rf_grid_trigger();
   rf_grid_wait();
-  const int add = w.n_new[b], len = w.old_len[b], page = len / kPage + blockIdx.x, t0 = page * kPage;
-  if (add == 0 || t0 >= len + add) return;
+  const int add = w.n_new[b], len = w.old_len[b], page = rf_append_page(len, add, blockIdx.x);
+  if (page < 0) return;
+  const int t0 = page * kPage;
   const int held = max(0, min(kPage, len - t0)), end = min(kPage, len + add - t0);
   const int dst = c.table[(size_t)b * c.max_pages + page];
   if (!rf_in_bounds(dst, c.n_pages, dev_status)) return;

@@ -26,7 +26,12 @@ struct RfQueries {
   const int32_t* q_len;         // null: M
 };
 
-__device__ __forceinline__ int rf_pages(int tokens) { return (tokens + kPage - 1) / kPage; }
+__host__ __device__ __forceinline__ int rf_pages(int tokens) { return (tokens + kPage - 1) / kPage; }
+// The page of a sequence that the x-th CTA of an append's grid writes to; -1: none.  (In pages: positions past a grid for 2^30 tokens pass 2^31.)
+__host__ __device__ __forceinline__ int rf_append_page(int len, int add, unsigned x) {
+  const int page = len / kPage + (int)x;
+  return add > 0 && page < rf_pages(len + add) ? page : -1;
+}
 
 // A sequence's length as read, made safe.
 __device__ __forceinline__ int rf_seq_len(const RfCache& c, int b, int32_t* dev_status) {
