@@ -403,6 +403,13 @@ def _cache_arg(name, t, dtype, shape, device):
     return t.data_ptr()
 
 
+def _int32(name, x):
+    """x, which ctypes would cut to its low 32 bits without a word."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise RainFusionError(f"{name} = {x}: an int32 is wanted")
+    return x
+
+
 class KVCache:
     """rf_cache over the caller's tensors: k, v float8_e4m3fn (or their bytes as uint8) [n_pages, heads, 128, D]; k_scale, v_scale float
     [n_pages, heads]; k_sum float [n_pages, heads, D]; page_table int32 [n_seqs, max_pages]; seq_len int32 [n_seqs].  KVCache.empty
@@ -415,7 +422,7 @@ class KVCache:
         n_pages, heads, _, D = k.shape
         n_seqs, max_pages = page_table.shape
         dev = k.device
-        self.c = rf_cache(n_seqs, heads, D, n_pages, max_pages, _cache_arg("k", k, k.dtype, k.shape, dev),
+        self.c = rf_cache(*(_int32("a dimension", x) for x in (n_seqs, heads, D, n_pages, max_pages)), _cache_arg("k", k, k.dtype, k.shape, dev),
                           _cache_arg("v", v, k.dtype, k.shape, dev), _cache_arg("k_scale", k_scale, torch.float32, (n_pages, heads), dev),
                           _cache_arg("v_scale", v_scale, torch.float32, (n_pages, heads), dev),
                           _cache_arg("k_sum", k_sum, torch.float32, (n_pages, heads, D), dev),
@@ -470,7 +477,8 @@ class KVCache:
         if key not in self._queries:
             if len(self._queries) >= 64:
                 self._queries.clear()
-            self._queries[key] = C.byref(rf_cache_query(H, M, causal_block, 0.0 if scale is None else scale))
+            self._queries[key] = C.byref(rf_cache_query(_int32("H", H), _int32("M", M), _int32("causal_block", causal_block),
+                                                         0.0 if scale is None else scale))
         return ptr, self._queries[key]
 
 
@@ -483,7 +491,8 @@ class CacheSchedule:
             raise RainFusionError("pages: [n_seqs, heads, nQ, capacity] is wanted")
         self.count, self.pages = count, pages
         self.c = rf_schedule(_cache_arg("count", count, torch.int32, pages.shape[:3], pages.device),
-                             _cache_arg("pages", pages, torch.int32, pages.shape, pages.device), None, None, pages.shape[2], pages.shape[3])
+                             _cache_arg("pages", pages, torch.int32, pages.shape, pages.device), None, None, _int32("nQ", pages.shape[2]),
+                             _int32("capacity", pages.shape[3]))
         self.ref = C.byref(self.c)
 
     @classmethod
@@ -496,7 +505,7 @@ class CacheSchedule:
 
 def alloc_cache_attn_workspace(cache: KVCache, H: int, M: int):
     import torch
-    query = rf_cache_query(H, M, 0, 0.0)
+    query = rf_cache_query(_int32("H", H), _int32("M", M), 0, 0.0)
     n = load().rf_cache_attn_workspace_bytes(cache.ref, C.byref(query))
     if n == 0:
         raise RainFusionError("rf_cache_attn_workspace_bytes: invalid or unsupported sizes")
@@ -535,7 +544,8 @@ def _cache_sched(cache, sched):
 def rf_cache_select(cache: KVCache, q, sched: CacheSchedule, q_len=None, causal_block=0, keep_first=0, keep_last=0, top_k=0, dev_status=None):
     """Fills sched with the pages that the tiles of query rows of q [n_seqs, H, M, D] attend to."""
     ptr, query = cache.query(q, causal_block, None)
-    _check(load().rf_cache_select(cache.ref, query, ptr, cache.ints("q_len", q_len), keep_first, keep_last, top_k, _cache_sched(cache, sched),
+    _check(load().rf_cache_select(cache.ref, query, ptr, cache.ints("q_len", q_len), _int32("keep_first", keep_first), _int32("keep_last", keep_last),
+                                  _int32("top_k", top_k), _cache_sched(cache, sched),
                                   cache.word("dev_status", dev_status), cache.stream()), "rf_cache_select")
 
 

@@ -1,0 +1,23 @@
+"""What the cache's binding refuses before it calls the library, on host tensors."""
+import pytest
+import torch
+
+from paper_2505_21036_b200 import api
+
+
+def test_numbers_that_do_not_fit_32_bits():
+    """Cut to 32 bits, 2**32 would be no mask at all and 2**32 + 5 pages five."""
+    c = api.KVCache.empty(1, 1, 64, 4, 4, "cpu")
+    q = torch.zeros((1, 1, 3, 64), dtype=torch.bfloat16)
+    o, sched = torch.empty_like(q), api.CacheSchedule.empty(c, 1, 3, 4)
+    for bad in (2 ** 32, 2 ** 32 + 5, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(api.RainFusionError, match="causal_block"):
+            api.rf_cache_attn_fwd(c, q, o, causal_block=bad)
+        with pytest.raises(api.RainFusionError, match="causal_block"):
+            api.rf_cache_select(c, q, sched, causal_block=bad, top_k=1)
+        for name in ("keep_first", "keep_last", "top_k"):
+            with pytest.raises(api.RainFusionError, match=name):
+                api.rf_cache_select(c, q, sched, **{name: bad})
+        with pytest.raises(api.RainFusionError, match="M = "):
+            api.alloc_cache_attn_workspace(c, 1, bad)
+    assert c.query(q, 2 ** 31 - 1, None)
