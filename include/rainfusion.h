@@ -419,8 +419,10 @@ rf_status rf_cache_compact(const rf_cache *cache, int32_t *n_live, void *ws, siz
  * Queries of a call on the cache.  q is bf16 [n_seqs, H, M, D]; H is a multiple of cache->heads, and heads g * H / heads .. of q
  * share K/V head g.  Sequence b has q_len[b] <= M query rows: the last q_len[b] tokens of the sequence (which are in the cache already),
  * row i at position p = seq_len[b] - q_len[b] + i.  Rows from q_len[b] on are padding: what they hold does not matter, and their outputs are not written.
- * With causal_block = c > 0 a row sees the keys of its own block of c positions and of the blocks before: positions below
- * (p / c + 1) * c (c = tokens of a frame: frame by frame; 1: token by token), none if p < 0.  c = 0: every key.
+ * With causal_block = c > 0 a row sees the keys of its own block of c positions and of the blocks before (c = tokens of a frame: frame by frame;
+ * 1: token by token), none if p < 0.  Blocks are counted from position 0 of what the cache holds now: a row sees positions below (p / c + 1) * c.
+ * Frames that begin elsewhere (behind a prompt; after rf_cache_drop has taken out tokens before them) want the entry points with a
+ * block_origin.  c = 0: every key.
  * The rows of a K/V head, [H / heads * M] one query head after the other, are cut into tiles of RF_CACHE_PAGE rows; a
  * schedule lists pages (entry c = tokens c * RF_CACHE_PAGE ..) per tile.
  */
@@ -443,6 +445,17 @@ rf_status rf_cache_select(const rf_cache *cache, const rf_cache_query *query, co
                           int32_t keep_last, int32_t top_k, rf_schedule *out, int32_t *dev_status, void *cuda_stream);
 
 /*
+ * rf_cache_select and rf_cache_attn_fwd with causal blocks that begin where the caller says.
+ *   block_origin   device int32 [n_seqs] or NULL (0 everywhere): blocks of c positions begin at o = block_origin[b], o + c, .., and what lies before o is
+ *                  one block more.  A row at p >= o sees positions below o + ((p - o) / c + 1) * c, a row at p < o those below o.  Any number will
+ *                  do: a negative one is a border that has been dropped.  After rf_cache_drop has taken out n tokens before the
+ *                  frames whose rows are to come, their borders are n positions lower.
+ */
+rf_status rf_cache_select_origin(const rf_cache *cache, const rf_cache_query *query, const void *q, const int32_t *q_len,
+                                 const int32_t *block_origin, int32_t keep_first, int32_t keep_last, int32_t top_k, rf_schedule *out,
+                                 int32_t *dev_status, void *cuda_stream);
+
+/*
  * Attention over the cache (Eq. 1-2 on the sequence's tokens), all pages or those that a schedule lists.
  *   q       device bf16 [n_seqs, H, M, D], 16-byte aligned; q_len device int32 [n_seqs] in 0..M or NULL (M rows everywhere)
  *   sched   NULL, or count / kv_tile as rf_cache_select writes them, or the caller's own (ascending, each page once; a page past
@@ -457,6 +470,9 @@ size_t rf_cache_attn_workspace_bytes(const rf_cache *cache, const rf_cache_query
 rf_status rf_cache_attn_fwd(const rf_cache *cache, const rf_cache_query *query, const void *q, const int32_t *q_len,
                             const rf_schedule *sched, void *o, float *lse, void *ws, size_t ws_bytes, int32_t *dev_status,
                             void *cuda_stream);
+rf_status rf_cache_attn_fwd_origin(const rf_cache *cache, const rf_cache_query *query, const void *q, const int32_t *q_len,
+                                   const int32_t *block_origin, const rf_schedule *sched, void *o, float *lse, void *ws, size_t ws_bytes,
+                                   int32_t *dev_status, void *cuda_stream);
 
 #ifdef __cplusplus
 }

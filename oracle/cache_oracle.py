@@ -40,6 +40,7 @@ class Cache:
         self.k_sum = np.zeros((n_pages, heads, D))
         self.rows = [[] for _ in range(n_seqs)]
         self.len = [0] * n_seqs
+        self.origin = [0] * n_seqs      # where a sequence's causal blocks begin: the caller's to keep
 
     def named(self):
         n = [0] * self.P
@@ -130,10 +131,12 @@ class Cache:
         return np.concatenate(x)[:self.len[b]] if x else np.zeros((0, self.D))
 
     def sees(self, b, q_len, causal):
-        """Keys that each of the q_len rows sees."""
-        L = self.len[b]
+        """Keys that each of the q_len rows sees: those up to the end of its block, where blocks end at the origin and every `causal` positions on."""
+        L, o = self.len[b], self.origin[b]
         p = [L - q_len + i for i in range(q_len)]
-        return [L if causal == 0 else (0 if x < 0 else min(L, (x // causal + 1) * causal)) for x in p]
+        if causal == 0:
+            return [L] * q_len
+        return [0 if x < 0 else min(L, o if x < o else o + ((x - o) // causal + 1) * causal) for x in p]
 
     def select(self, q, q_len, causal, keep_first, keep_last, top_k):
         """q [B, H, M, D]; lists [b][g][tile]."""

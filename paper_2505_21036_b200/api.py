@@ -26,7 +26,7 @@ EXPORTS = ["rf_status_string", "rf_schedule_dims", "rf_workspace_bytes", "rf_arm
            "rf_host_pipeline_create", "rf_host_pipeline_run", "rf_host_pipeline_status", "rf_host_pipeline_destroy",
            "rf_host_pipeline_set_bandwidths", "rf_host_pipeline_head_class", "rf_host_pipeline_head_window",
            "rf_cache_workspace_bytes", "rf_cache_append", "rf_cache_fork", "rf_cache_drop", "rf_cache_compact", "rf_cache_select",
-           "rf_cache_attn_workspace_bytes", "rf_cache_attn_fwd"]
+           "rf_cache_attn_workspace_bytes", "rf_cache_attn_fwd", "rf_cache_select_origin", "rf_cache_attn_fwd_origin"]
 CACHE_PAGE = 128
 
 
@@ -145,6 +145,10 @@ def load():
     lib.rf_cache_attn_workspace_bytes.argtypes = [P(rf_cache), P(rf_cache_query)]
     lib.rf_cache_attn_fwd.restype = I
     lib.rf_cache_attn_fwd.argtypes = [P(rf_cache), P(rf_cache_query), V, V, P(rf_schedule), V, V, V, Z, V, V]
+    lib.rf_cache_select_origin.restype = I
+    lib.rf_cache_select_origin.argtypes = [P(rf_cache), P(rf_cache_query), V, V, V, C.c_int32, C.c_int32, C.c_int32, P(rf_schedule), V, V]
+    lib.rf_cache_attn_fwd_origin.restype = I
+    lib.rf_cache_attn_fwd_origin.argtypes = [P(rf_cache), P(rf_cache_query), V, V, V, P(rf_schedule), V, V, V, Z, V, V]
     _lib = lib
     return lib
 
@@ -541,24 +545,27 @@ def _cache_sched(cache, sched):
     return sched.ref
 
 
-def rf_cache_select(cache: KVCache, q, sched: CacheSchedule, q_len=None, causal_block=0, keep_first=0, keep_last=0, top_k=0, dev_status=None):
-    """Fills sched with the pages that the tiles of query rows of q [n_seqs, H, M, D] attend to."""
+def rf_cache_select(cache: KVCache, q, sched: CacheSchedule, q_len=None, causal_block=0, keep_first=0, keep_last=0, top_k=0, dev_status=None,
+                    block_origin=None):
+    """Fills sched with the pages that the tiles of query rows of q [n_seqs, H, M, D] attend to.  block_origin: int32 [n_seqs] on the device, the
+    positions where the causal blocks begin, or None for 0."""
     ptr, query = cache.query(q, causal_block, None)
-    _check(load().rf_cache_select(cache.ref, query, ptr, cache.ints("q_len", q_len), _int32("keep_first", keep_first), _int32("keep_last", keep_last),
-                                  _int32("top_k", top_k), _cache_sched(cache, sched),
-                                  cache.word("dev_status", dev_status), cache.stream()), "rf_cache_select")
+    _check(load().rf_cache_select_origin(cache.ref, query, ptr, cache.ints("q_len", q_len), cache.ints("block_origin", block_origin),
+                                         _int32("keep_first", keep_first), _int32("keep_last", keep_last), _int32("top_k", top_k),
+                                         _cache_sched(cache, sched), cache.word("dev_status", dev_status), cache.stream()), "rf_cache_select")
 
 
 def rf_cache_attn_fwd(cache: KVCache, q, o, lse=None, sched: Optional[CacheSchedule] = None, q_len=None, causal_block=0, scale=None, ws=None,
-                      dev_status=None):
-    """q, o: bf16 [n_seqs, H, M, D]; lse: float [n_seqs, H, M] or None; ws: alloc_cache_attn_workspace(cache, H, M), by default a block
-    from torch's allocator for the time of the call."""
+                      dev_status=None, block_origin=None):
+    """q, o: bf16 [n_seqs, H, M, D]; lse: float [n_seqs, H, M] or None; scale: 1 / sqrt(D) where None or 0; ws: alloc_cache_attn_workspace(cache, H,
+    M), by default a block from torch's allocator for the time of the call; block_origin: int32 [n_seqs] on the device, the positions where the
+    causal blocks begin, or None for 0."""
     ptr, query = cache.query(q, causal_block, scale)
     if ws is None:
         ws = alloc_cache_attn_workspace(cache, q.shape[1], q.shape[2])
     if ws.device != cache.device:
         raise RainFusionError("ws is not on the cache's device")
-    _check(load().rf_cache_attn_fwd(cache.ref, query, ptr, cache.ints("q_len", q_len), None if sched is None else _cache_sched(cache, sched),
-                                    _cache_arg("o", o, cache._bf16, q.shape, cache.device),
-                                    _cache_arg("lse", lse, cache._float, q.shape[:3], cache.device), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                    cache.word("dev_status", dev_status), cache.stream()), "rf_cache_attn_fwd")
+    _check(load().rf_cache_attn_fwd_origin(cache.ref, query, ptr, cache.ints("q_len", q_len), cache.ints("block_origin", block_origin),
+                                           None if sched is None else _cache_sched(cache, sched), _cache_arg("o", o, cache._bf16, q.shape, cache.device),
+                                           _cache_arg("lse", lse, cache._float, q.shape[:3], cache.device), ws.data_ptr(),
+                                           ws.numel() * ws.element_size(), cache.word("dev_status", dev_status), cache.stream()), "rf_cache_attn_fwd")

@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) rf_cache_select_kernel(RfCache
   const int tile = blockIdx.x * T + mine, h = blockIdx.y, b = blockIdx.z;
   rf_grid_wait();
   const int len = rf_seq_len(c, b, dev_status), q_len = rf_query_len(u, b, dev_status);
-  const int sees = tile < u.n_q ? rf_rows_see(u, len, q_len, tile * kPage, kPage) : -1;
+  const int sees = tile < u.n_q ? rf_rows_see(u, rf_origin(u, b), len, q_len, tile * kPage, kPage) : -1;
   const size_t row = ((size_t)b * c.H + h) * u.n_q + min(tile, u.n_q - 1);
   const int n = min(rf_pages(max(sees, 0)), kSelectMaxPages);             // pages in which some row of the tile sees a key
   const int first_end = min(keep_first, n), last_begin = max(n - min(keep_last, n), first_end);

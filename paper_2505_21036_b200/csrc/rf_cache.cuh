@@ -24,6 +24,7 @@ struct RfQueries {
   int causal;                   // tokens of a causal block, 0: none
   const __nv_bfloat16* q;       // [B, H, G * M, D]
   const int32_t* q_len;         // null: M
+  const int32_t* origin;        // where the causal blocks begin, null: 0
 };
 
 __host__ __device__ __forceinline__ int rf_pages(int tokens) { return (tokens + kPage - 1) / kPage; }
@@ -47,23 +48,24 @@ __device__ __forceinline__ int rf_query_len(const RfQueries& u, int b, int32_t* 
   rf_report(dev_status, RF_ERR_INVALID_ARG);
   return n < 0 ? 0 : u.M;
 }
-// Keys that query row i of a head sees.
-__device__ __forceinline__ int rf_row_sees(int causal, int len, int q_len, int i) {
+__device__ __forceinline__ int rf_origin(const RfQueries& u, int b) { return u.origin == nullptr ? 0 : u.origin[b]; }
+// Keys that query row i of a head sees.  Blocks of `causal` positions begin at `origin`, which may be any number; what lies before it is a block too.
+__host__ __device__ __forceinline__ int rf_row_sees(int causal, int origin, int len, int q_len, int i) {
   if (causal == 0) return len;
   const int p = len - q_len + i;
   if (p < 0) return 0;
-  const long long end = ((long long)(p / causal) + 1) * causal;
+  const long long end = p < origin ? origin : (long long)origin + ((long long)(((unsigned)p - (unsigned)origin) / (unsigned)causal) + 1) * causal;
   return (int)(end < len ? end : (long long)len);
 }
 // (Out of line: two divisions, and its callers' code is to stay short.)  The most keys that any of the rows [r0, r0 + n) of a K/V head sees (they grow with a row's place in its head); -1 if
 // all of them are padding.  Row r is row r % M of its query head.
-static __device__ __noinline__ int rf_rows_see(const RfQueries& u, int len, int q_len, int r0, int n) {
+static __host__ __device__ __noinline__ int rf_rows_see(const RfQueries& u, int origin, int len, int q_len, int r0, int n) {
   int i0 = r0, last;                               // the last place in a head among the rows that are there
   if (u.G != 1) i0 = r0 % u.M;
-  const int end = i0 + min(n, u.rows - r0);
-  if (end <= u.M) last = i0 < q_len ? min(end, q_len) - 1 : -1;
+  const int end = i0 + (n < u.rows - r0 ? n : u.rows - r0);
+  if (end <= u.M) last = i0 < q_len ? (end < q_len ? end : q_len) - 1 : -1;
   else last = i0 < q_len || end >= u.M + q_len ? q_len - 1 : end - u.M - 1;
-  return last < 0 ? -1 : rf_row_sees(u.causal, len, q_len, last);
+  return last < 0 ? -1 : rf_row_sees(u.causal, origin, len, q_len, last);
 }
 
 // Physical page of a sequence's page c, made safe.

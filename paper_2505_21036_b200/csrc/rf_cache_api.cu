@@ -25,7 +25,7 @@ rf_status check_query(const RfCache& c, const rf_cache_query* u, RfQueries* out)
   if (u == nullptr || u->H < 1 || u->M < 1 || u->causal_block < 0 || !(u->scale >= 0.f && isfinite(u->scale)) || u->H % c.H != 0) return RF_ERR_INVALID_ARG;
   const long long rows = (long long)(u->H / c.H) * u->M;
   if (rows > (1ll << 30) || (long long)c.B * c.H * ((rows + 15) / 16) > (1ll << 30)) return RF_ERR_UNSUPPORTED;
-  *out = RfQueries{u->M, u->H / c.H, (int)rows, (int)((rows + kPage - 1) / kPage), u->causal_block, nullptr, nullptr};
+  *out = RfQueries{u->M, u->H / c.H, (int)rows, (int)((rows + kPage - 1) / kPage), u->causal_block, nullptr, nullptr, nullptr};
   return RF_OK;
 }
 
@@ -87,6 +87,12 @@ rf_status rf_cache_compact(const rf_cache* cache, int32_t* n_live, void* ws, siz
 
 rf_status rf_cache_select(const rf_cache* cache, const rf_cache_query* query, const void* q, const int32_t* q_len, int32_t keep_first,
                           int32_t keep_last, int32_t top_k, rf_schedule* out, int32_t* dev_status, void* cuda_stream) {
+  return rf_cache_select_origin(cache, query, q, q_len, nullptr, keep_first, keep_last, top_k, out, dev_status, cuda_stream);
+}
+
+rf_status rf_cache_select_origin(const rf_cache* cache, const rf_cache_query* query, const void* q, const int32_t* q_len,
+                                 const int32_t* block_origin, int32_t keep_first, int32_t keep_last, int32_t top_k, rf_schedule* out,
+                                 int32_t* dev_status, void* cuda_stream) {
   RfCache c;
   RfQueries u;
   rf_status st = check_cache(cache, &c);
@@ -99,6 +105,7 @@ rf_status rf_cache_select(const rf_cache* cache, const rf_cache_query* query, co
   if (c.max_pages > kSelectMaxPages) return RF_ERR_UNSUPPORTED;
   u.q = static_cast<const __nv_bfloat16*>(q);
   u.q_len = q_len;
+  u.origin = block_origin;
   return done(rf_launch_cache_select(c, u, keep_first, keep_last, top_k, out->count, out->kv_tile, out->nKmax, dev_status,
                                      static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -111,6 +118,12 @@ size_t rf_cache_attn_workspace_bytes(const rf_cache* cache, const rf_cache_query
 
 rf_status rf_cache_attn_fwd(const rf_cache* cache, const rf_cache_query* query, const void* q, const int32_t* q_len, const rf_schedule* sched,
                             void* o, float* lse, void* ws, size_t ws_bytes, int32_t* dev_status, void* cuda_stream) {
+  return rf_cache_attn_fwd_origin(cache, query, q, q_len, nullptr, sched, o, lse, ws, ws_bytes, dev_status, cuda_stream);
+}
+
+rf_status rf_cache_attn_fwd_origin(const rf_cache* cache, const rf_cache_query* query, const void* q, const int32_t* q_len,
+                                   const int32_t* block_origin, const rf_schedule* sched, void* o, float* lse, void* ws, size_t ws_bytes,
+                                   int32_t* dev_status, void* cuda_stream) {
   RfCacheAttn a = {};
   rf_status st = check_cache(cache, &a.c);
   if (st == RF_OK) st = check_query(a.c, query, &a.u);
@@ -126,6 +139,7 @@ rf_status rf_cache_attn_fwd(const rf_cache* cache, const rf_cache_query* query, 
   if (st != RF_OK) return st;
   a.u.q = static_cast<const __nv_bfloat16*>(q);
   a.u.q_len = q_len;
+  a.u.origin = block_origin;
   a.o = static_cast<__nv_bfloat16*>(o);
   a.lse = lse;
   a.scale_log2 = (query->scale != 0.f ? query->scale : 1.f / sqrtf((float)a.c.D)) * 1.4426950408889634f;

@@ -31,7 +31,7 @@ template <int kRows>
 static __device__ __noinline__ TokenItem token_item(const RfCacheAttn& a, int item) {
   TokenItem t;
   t.it = cache_item<kRows>(a, item);
-  const int sees = rf_rows_see(a.u, t.it.len, t.it.q_len, t.it.r0, kRows);
+  const int sees = rf_rows_see(a.u, t.it.origin, t.it.len, t.it.q_len, t.it.r0, kRows);
   t.tiles = sees < 0 ? -1 : a.count == nullptr ? rf_pages(sees) : listed(a, t.it, t.it.r0 / kPage);
   return t;
 }
@@ -45,7 +45,7 @@ struct Cfg {
   static constexpr uint32_t SUMS = JOIN + WARPS * ROWS * D * 4;     // [WARPS][ROWS] {m, l, l of the unrounded weights}
   static constexpr uint32_t BAR = SUMS + WARPS * ROWS * 16;
   static constexpr uint32_t REC = BAR + 8 * (2 * SLOTS + 2);
-  static constexpr uint32_t MISC = REC + SLOTS * 32;
+  static constexpr uint32_t MISC = REC + SLOTS * 32;                // (a Record each)
   static constexpr uint32_t TOTAL = MISC + 16 + sizeof(StretchScratch<TokenItem>);
   static constexpr uint32_t ALLOC = TOTAL + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory of a CTA");
@@ -56,7 +56,8 @@ struct Cfg {
   }
 };
 
-struct Record { int item, page, flags, len, q_len; float ks, vs; };
+struct Record { int item, page, flags, len, q_len, origin; float ks, vs; };
+static_assert(sizeof(Record) == 32, "Cfg::REC");
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -132,7 +133,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       const int n = sent[group], s = group * C::STAGES + n % C::STAGES;
       if (!wait_for(empty(s), ((n / C::STAGES) & 1) ^ 1, wc)) return;        // (the first round finds them free) abandoned: nothing more is fetched
       volatile Record* d = records + s;
-      d->item = r.item; d->page = r.page; d->flags = r.flags; d->len = r.len; d->q_len = r.q_len;
+      d->item = r.item; d->page = r.page; d->flags = r.flags; d->len = r.len; d->q_len = r.q_len; d->origin = r.origin;
       d->ks = r.ks; d->vs = r.vs;
       if (bytes) {
         const uint32_t to = base + s * 2 * C::TILE;
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
 #pragma unroll 1
         for (int i = 0; i < batch; ++i) {
           Record s;
-          s.item = item; s.len = it.len; s.q_len = it.q_len;
+          s.item = item; s.len = it.len; s.q_len = it.q_len; s.origin = it.origin;
           s.page = __shfl_sync(0xffffffffu, r.page, i);
           s.flags = __shfl_sync(0xffffffffu, r.flags, i);
           s.ks = __shfl_sync(0xffffffffu, r.ks, i);
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
     }
     if (lane == 0)
 #pragma unroll 1
-      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0, 0, 0.f, 0.f}, g, false, 0);
+      for (int g = 0; g < C::GROUPS; ++g) publish(Record{0, 0, kEnd, 0, 0, 0, 0.f, 0.f}, g, false, 0);
   } else {
     // ------------------------------------------------------------ consumers: 16 keys of every tile of their group each
     const int g = lane >> 2, t = lane & 3, group = warp >> 3, slice = 16 * (warp & 7);
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
       Record rec;
       {
         volatile const Record* r = records + slot;
-        rec.item = r->item; rec.page = r->page; rec.flags = r->flags; rec.len = r->len; rec.q_len = r->q_len;
+        rec.item = r->item; rec.page = r->page; rec.flags = r->flags; rec.len = r->len; rec.q_len = r->q_len; rec.origin = r->origin;
         rec.ks = r->ks; rec.vs = r->vs;
       }
       if (rec.flags & kEnd) break;
@@ -227,11 +228,12 @@ __global__ void __launch_bounds__((Cfg<D, NB>::THREADS), 1) rf_cache_token_kerne
         it.r0 = 0;
         it.len = rec.len;
         it.q_len = rec.q_len;
+        it.origin = rec.origin;
         const __nv_bfloat16* src = a.u.q + (size_t)it.bh * a.u.rows * D;
         int row_sees = -1;                                         // keys that row `lane` sees; -1: it is not there
         if (lane < kRows && it.r0 + lane < a.u.rows) {
           const int place = (it.r0 + lane) % a.u.M;
-          if (place < it.q_len) row_sees = rf_row_sees(a.u.causal, it.len, it.q_len, place);
+          if (place < it.q_len) row_sees = rf_row_sees(a.u.causal, it.origin, it.len, it.q_len, place);
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {

@@ -28,7 +28,7 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, const sm
 }
 
 // An item: rows [r0, r0 + kRows) of K/V head bh.
-struct CacheItem { int b, bh, r0, len, q_len; };
+struct CacheItem { int b, bh, r0, len, q_len, origin; };
 template <int kRows>
 __device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) {
   const int blocks = rf_cdiv(a.u.rows, kRows);
@@ -38,6 +38,7 @@ __device__ __forceinline__ CacheItem cache_item(const RfCacheAttn& a, int item) 
   it.b = it.bh / a.c.H;
   it.len = rf_seq_len(a.c, it.b, a.dev_status);
   it.q_len = rf_query_len(a.u, it.b, a.dev_status);
+  it.origin = rf_origin(a.u, it.b);
   return it;
 }
 // Entries of the list of a tile of query rows.

@@ -82,7 +82,7 @@ static __device__ __noinline__ ChunkItem chunk_item(const RfCacheAttn& a, int it
   c.there = false;
 #pragma unroll 1
   for (int j = 0; j < 2; ++j) {
-    const int r = c.it.r0 + j * BM, sees = r < a.u.rows ? rf_rows_see(a.u, c.it.len, c.it.q_len, r, BM) : -1;
+    const int r = c.it.r0 + j * BM, sees = r < a.u.rows ? rf_rows_see(a.u, c.it.origin, c.it.len, c.it.q_len, r, BM) : -1;
     c.there |= sees >= 0;
     const int tiles = sees < 0 ? 0 : a.count == nullptr ? rf_pages(sees) : rf_cache_attn::listed(a, c.it, r / kPage);
     if (j == 0) n[0] = tiles; else n[1] = tiles;
@@ -390,6 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
         if (lane == 0) {
           int* w = items + slot * kItemWords;
           w[0] = it.bh; w[1] = it.r0; w[2] = it.len; w[3] = it.q_len; w[4] = pages; w[5] = e0 - b0; w[6] = e1 - b1; w[7] = b0; w[8] = b1;
+          w[10] = it.origin;
           w[9] = (begin > 0 ? kHeadPiece : 0) | (end < n && begin == 0 ? kTailPiece : 0);
           mbar_arrive(bar(C::B_IF + slot));
         }
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) rf_cache_chunk_kernel(const __gri
       waited = iw[5] + iw[6];
       const int r = iw[1] + j * BM + row_in_tile;
       int sees = 0;                                       // keys that this row sees; none if it is padding
-      if (r < a.u.rows && r % a.u.M < iw[3]) sees = rf_row_sees(a.u.causal, iw[2], iw[3], r % a.u.M);
+      if (r < a.u.rows && r % a.u.M < iw[3]) sees = rf_row_sees(a.u.causal, iw[10], iw[2], iw[3], r % a.u.M);
       const int32_t* list = a.count != nullptr ? a.pages + ((size_t)iw[0] * a.u.n_q + min(iw[1] / kPage + j, a.u.n_q - 1)) * a.n_k : nullptr;
       float m_run = -INFINITY, l_run = 0.f, l_exact = 0.f;
       int ref_run = 0;                                    // O is in units of 2^ref_run
