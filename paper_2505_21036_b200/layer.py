@@ -92,7 +92,9 @@ class StreamingAttention:
       layer.begin_chunk()
       for step in range(num_steps):
           layer(q, k, v, o, step=step, num_steps=num_steps)    # the step's K and V replace the last step's in the cache
-      # the last step's stay; further operations between chunks: fork, drop, compact
+      # the last step's stay; further operations, between chunks or between steps: fork, drop, compact
+
+    What the cache holds when the layer is made belongs to finished chunks.
 
     The first `dense_fraction` of the steps attend to every page; with `top_k` set, the others attend to the pages that are selected
     for every 128 query rows (the first `keep_first` and last `keep_last` always: prompt and first frame, the chunk itself and its
@@ -105,7 +107,7 @@ class StreamingAttention:
             raise ValueError("dense_fraction must be in [0, 1]")
         self.cache, self.heads, self.chunk_tokens, self.causal_block = cache, heads, chunk_tokens, causal_block
         self.top_k, self.keep_first, self.keep_last, self.dense_fraction = top_k, keep_first, keep_last, dense_fraction
-        self.base = torch.zeros_like(cache.seq_len)
+        self.base = cache.seq_len.clone()              # tokens of finished chunks: where the chunk begins
         self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
         self.live = torch.zeros(1, dtype=torch.int32, device=cache.device)
         self.ws = api.alloc_cache_attn_workspace(cache, heads, chunk_tokens)
@@ -131,12 +133,21 @@ class StreamingAttention:
         api.rf_cache_attn_fwd(self.cache, q, o, lse, sched, new_len, self.causal_block, None, self.ws, self.status)
 
     def fork(self, parent):
-        """Every sequence b continues sequence parent[b] (int32 on the device; -1: it ends)."""
+        """Every sequence b continues sequence parent[b] (int32 on the device; -1: it ends), its unfinished chunk included."""
+        before = self.cache.seq_len.clone()
         api.rf_cache_fork(self.cache, parent, self.status)
+        # a call that the library refuses changes nothing here either
+        valid = ((parent >= -1) & (parent < self.cache.n_seqs) & (before >= 0) & (before <= self.cache.max_pages * api.CACHE_PAGE)).all()
+        source = parent.clamp(0, self.cache.n_seqs - 1).long()
+        self.base.copy_(self.base.where(~valid, self.base[source].where(parent >= 0, 0)))
 
     def drop(self, first, count):
         """Sequence b lets go of its pages [first[b], first[b] + count[b]): a window that slides."""
+        before = self.cache.seq_len.long()
         api.rf_cache_drop(self.cache, first, count, None, self.status)
+        gone = before - self.cache.seq_len                         # tokens [start, start + gone); none if the library refused
+        start = first.long() * api.CACHE_PAGE
+        self.base -= ((start + gone).minimum(self.base) - start).clamp(min=0).int()
 
     def compact(self):
         """Pages in use move to the front of the pool; returns how many there are (on the device)."""
