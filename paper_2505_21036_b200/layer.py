@@ -14,6 +14,7 @@ arithmetic step is a kernel of the library.
 from __future__ import annotations
 
 import math
+import warnings
 
 from . import api
 
@@ -98,16 +99,29 @@ class StreamingAttention:
 
     The first `dense_fraction` of the steps attend to every page; with `top_k` set, the others attend to the pages that are selected
     for every 128 query rows (the first `keep_first` and last `keep_last` always: prompt and first frame, the chunk itself and its
-    neighbours).  Everything that varies between steps is on the device, so a step can be captured into a graph."""
+    neighbours).  Everything that varies between steps is on the device, so a step can be captured into a graph.
+
+    With `causal_block` a row attends to its own block of that many tokens and to what lies before it.  Frames want `prompt_tokens` too: how many
+    tokens stand in front of a sequence's first frame (a number, or int32 [n_seqs]; 0 where there is no prompt).  The blocks are then the
+    clip's frames, counted from the end of the prompt: fork and drop carry their borders along, and begin_chunk can set a new one.  Without it
+    they are blocks of positions in the cache as it is now, counted from its first token, whatever has been dropped before it."""
 
     def __init__(self, cache: api.KVCache, heads: int, chunk_tokens: int, causal_block: int = 0, top_k=None, keep_first: int = 0,
-                 keep_last: int = 0, dense_fraction: float = 0.1):
+                 keep_last: int = 0, dense_fraction: float = 0.1, prompt_tokens=None):
         import torch
         if not (0.0 <= dense_fraction <= 1.0):
             raise ValueError("dense_fraction must be in [0, 1]")
         self.cache, self.heads, self.chunk_tokens, self.causal_block = cache, heads, chunk_tokens, causal_block
         self.top_k, self.keep_first, self.keep_last, self.dense_fraction = top_k, keep_first, keep_last, dense_fraction
         self.base = cache.seq_len.clone()              # tokens of finished chunks: where the chunk begins
+        # where the frames begin for the chunk that begins at base, and where they do in a sequence that starts anew (fork's -1)
+        self.origin = self.first_origin = None
+        if prompt_tokens is not None:
+            if causal_block <= 0:
+                raise ValueError("prompt_tokens says where causal blocks begin: causal_block is wanted too")
+            self.first_origin = torch.as_tensor(prompt_tokens, dtype=torch.int32, device=cache.device).expand(cache.n_seqs).contiguous()
+            self.origin = self.first_origin.clone()
+            self.gone = torch.zeros_like(self.origin)  # tokens from base on that drop took out since the last step
         self.status = torch.zeros(1, dtype=torch.int32, device=cache.device)
         self.live = torch.zeros(1, dtype=torch.int32, device=cache.device)
         self.ws = api.alloc_cache_attn_workspace(cache, heads, chunk_tokens)
@@ -117,20 +131,36 @@ class StreamingAttention:
     def is_dense_step(self, step: int, num_steps: int) -> bool:
         return self.top_k is None or step < int(math.ceil(self.dense_fraction * num_steps - 1e-9))
 
-    def begin_chunk(self):
-        """What the cache holds now belongs to finished chunks."""
+    def begin_chunk(self, new_frame: bool = False):
+        """What the cache holds now belongs to finished chunks.  new_frame: the chunk begins a frame, also where the last one ended short."""
+        if new_frame and self.origin is None:
+            raise ValueError("frames are counted where prompt_tokens is given")
         self.base.copy_(self.cache.seq_len)
+        if new_frame:
+            self.origin.copy_(self.base)
+        elif self.origin is not None:
+            self._move_origin(self.gone)
+        if self.origin is not None:
+            self.gone.zero_()
+
+    def _move_origin(self, n):
+        """Borders move n[b] positions down, with the tokens behind them.  One that is no longer there stands for those whole frames behind it."""
+        moved = self.origin - n
+        self.origin.copy_(moved.where(moved >= 0, moved.remainder(self.causal_block)))
 
     def __call__(self, q, k, v, o, lse=None, new_len=None, step: int = 0, num_steps: int = 1):
         """q, o [n_seqs, heads, chunk_tokens, D], k, v [n_seqs, cache.heads, chunk_tokens, D]; new_len: int32 [n_seqs] on the device, tokens
         that each sequence's chunk really has (None: chunk_tokens)."""
         api.rf_cache_drop(self.cache, max_len=self.base, dev_status=self.status)
         api.rf_cache_append(self.cache, k, v, new_len, self.status)
+        if self.origin is not None:
+            self.gone.zero_()                          # the chunk is whole again
         sched = None
         if not self.is_dense_step(step, num_steps):
             sched = self.sched
-            api.rf_cache_select(self.cache, q, sched, new_len, self.causal_block, self.keep_first, self.keep_last, self.top_k, self.status)
-        api.rf_cache_attn_fwd(self.cache, q, o, lse, sched, new_len, self.causal_block, None, self.ws, self.status)
+            api.rf_cache_select(self.cache, q, sched, new_len, self.causal_block, self.keep_first, self.keep_last, self.top_k, self.status,
+                                self.origin)
+        api.rf_cache_attn_fwd(self.cache, q, o, lse, sched, new_len, self.causal_block, None, self.ws, self.status, self.origin)
 
     def fork(self, parent):
         """Every sequence b continues sequence parent[b] (int32 on the device; -1: it ends), its unfinished chunk included."""
@@ -139,15 +169,23 @@ class StreamingAttention:
         # a call that the library refuses changes nothing here either
         valid = ((parent >= -1) & (parent < self.cache.n_seqs) & (before >= 0) & (before <= self.cache.max_pages * api.CACHE_PAGE)).all()
         source = parent.clamp(0, self.cache.n_seqs - 1).long()
-        self.base.copy_(self.base.where(~valid, self.base[source].where(parent >= 0, 0)))
+        for x, empty in ((self.base, 0),) if self.origin is None else ((self.base, 0), (self.gone, 0), (self.origin, self.first_origin)):
+            x.copy_(x.where(~valid, x[source].where(parent >= 0, empty)))
 
     def drop(self, first, count):
         """Sequence b lets go of its pages [first[b], first[b] + count[b]): a window that slides."""
+        if self.causal_block > 0 and self.origin is None and api.CACHE_PAGE % self.causal_block != 0:
+            warnings.warn("StreamingAttention: causal blocks of cache positions are no frames behind dropped pages; give prompt_tokens (0 without a prompt)",
+                          stacklevel=2)
         before = self.cache.seq_len.long()
         api.rf_cache_drop(self.cache, first, count, None, self.status)
         gone = before - self.cache.seq_len                         # tokens [start, start + gone); none if the library refused
         start = first.long() * api.CACHE_PAGE
-        self.base -= ((start + gone).minimum(self.base) - start).clamp(min=0).int()
+        finished = ((start + gone).minimum(self.base) - start).clamp(min=0).int()
+        self.base -= finished
+        if self.origin is not None:
+            self._move_origin(finished)
+            self.gone += gone.int() - finished                     # the chunk's own: back with the next step, or finished with begin_chunk
 
     def compact(self):
         """Pages in use move to the front of the pool; returns how many there are (on the device)."""
