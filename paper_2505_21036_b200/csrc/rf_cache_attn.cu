@@ -71,10 +71,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 t = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&t);
-}
 constexpr float kWeightUnit = 32768.f;           // the weights' largest
 
 __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {

@@ -137,4 +137,8 @@ __device__ __forceinline__ uint32_t widen_high(uint32_t x) {
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(d) : "r"(x));
   return d;
 }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 t = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
 }  // namespace rf_cache_attn

@@ -41,6 +41,7 @@ using rf_cache_attn::Stretch;
 using rf_cache_attn::StretchScratch;
 using rf_cache_attn::head_floats;
 using rf_cache_attn::kHeadWords;
+using rf_cache_attn::pack_f16;
 using rf_cache_attn::widen_high;
 using rf_cache_attn::widen_low;
 
@@ -144,10 +145,6 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 t = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&t);
 }
 // 2^e for e <= 127, as far down as there are subnormal numbers.
 __device__ __forceinline__ float pow2i(int e) {
