@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Optional
 
@@ -477,12 +478,11 @@ class KVCache:
             raise RainFusionError("q: [n_seqs, H, M, D] is wanted")
         H, M = q.shape[1], q.shape[2]
         ptr = _cache_arg("q", q, self._bf16, (self.n_seqs, H, M, self.D), self.device)
-        key = (H, M, causal_block, scale)
+        key = (H, M, operator.index(causal_block), 0.0 if scale is None else float(scale))      # (numbers: a tensor of one is known by its identity)
         if key not in self._queries:
             if len(self._queries) >= 64:
                 self._queries.clear()
-            self._queries[key] = C.byref(rf_cache_query(_int32("H", H), _int32("M", M), _int32("causal_block", causal_block),
-                                                         0.0 if scale is None else scale))
+            self._queries[key] = C.byref(rf_cache_query(_int32("H", H), _int32("M", M), _int32("causal_block", key[2]), key[3]))
         return ptr, self._queries[key]
 
 

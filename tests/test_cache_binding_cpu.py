@@ -21,3 +21,20 @@ def test_numbers_that_do_not_fit_32_bits():
         with pytest.raises(api.RainFusionError, match="M = "):
             api.alloc_cache_attn_workspace(c, 1, bad)
     assert c.query(q, 2 ** 31 - 1, None)
+
+
+def test_a_scale_that_changes_in_place():
+    """The query's sizes are kept from call to call by their values, not by the object that held them."""
+    c = api.KVCache.empty(1, 1, 64, 4, 4, "cpu")
+    q = torch.zeros((1, 1, 3, 64), dtype=torch.bfloat16)
+    scale, block = torch.tensor(0.25), torch.tensor(7)
+    first = c.query(q, block, scale)[1]._obj
+    assert (first.scale, first.causal_block) == (0.25, 7)
+    scale.fill_(0.5)
+    block.fill_(9)
+    now = c.query(q, block, scale)[1]._obj
+    assert (now.scale, now.causal_block) == (0.5, 9)
+    assert c.query(q, 9, 0.5)[1]._obj is now and c.query(q, 9, None)[1]._obj.scale == 0.0
+    for bad in (7.5, "7"):
+        with pytest.raises(TypeError):
+            c.query(q, bad, None)
