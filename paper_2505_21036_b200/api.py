@@ -563,8 +563,8 @@ def rf_cache_attn_fwd(cache: KVCache, q, o, lse=None, sched: Optional[CacheSched
     ptr, query = cache.query(q, causal_block, scale)
     if ws is None:
         ws = alloc_cache_attn_workspace(cache, q.shape[1], q.shape[2])
-    if ws.device != cache.device:
-        raise RainFusionError("ws is not on the cache's device")
+    if ws.device != cache.device or not ws.is_contiguous():
+        raise RainFusionError("ws: a contiguous tensor on the cache's device is wanted")
     _check(load().rf_cache_attn_fwd_origin(cache.ref, query, ptr, cache.ints("q_len", q_len), cache.ints("block_origin", block_origin),
                                            None if sched is None else _cache_sched(cache, sched), _cache_arg("o", o, cache._bf16, q.shape, cache.device),
                                            _cache_arg("lse", lse, cache._float, q.shape[:3], cache.device), ws.data_ptr(),

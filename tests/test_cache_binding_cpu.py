@@ -38,3 +38,12 @@ def test_a_scale_that_changes_in_place():
     for bad in (7.5, "7"):
         with pytest.raises(TypeError):
             c.query(q, bad, None)
+
+
+def test_a_workspace_with_gaps():
+    """Its bytes would be counted without the gaps and written with them."""
+    c = api.KVCache.empty(1, 1, 64, 4, 4, "cpu")
+    q = torch.zeros((1, 1, 3, 64), dtype=torch.bfloat16)
+    whole = api.alloc_cache_attn_workspace(c, 1, 3)
+    with pytest.raises(api.RainFusionError, match="contiguous"):
+        api.rf_cache_attn_fwd(c, q, torch.empty_like(q), ws=torch.empty(2 * whole.numel(), dtype=torch.uint8)[::2])
