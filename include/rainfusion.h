@@ -356,8 +356,9 @@ rf_status rf_arm_classify_noalloc(const rf_shape *shape, const rf_params *params
  * Calls that write to a cache and calls that read it are ordered by the caller (one stream, or events), like any buffer's.
  * Limits: D in {64, 96, 128}; n_seqs <= 1024; heads * n_seqs <= 65535; n_pages <= 524288; n_pages * heads < 2^31; max_pages <= 2^23.
  * The first call of each kind on a device sets kernel attributes: make it outside any stream capture.
- * seq_len outside 0..max_pages * RF_CACHE_PAGE or a page number outside 0..n_pages-1 is reported as RF_ERR_INVALID_ARG through
- * dev_status: calls that write then change nothing, calls that read give arbitrary results for that sequence.
+ * seq_len outside 0..max_pages * RF_CACHE_PAGE is reported as RF_ERR_INVALID_ARG through dev_status, and so is a page number outside
+ * 0..n_pages-1, by the calls that look at it (rf_cache_append and rf_cache_compact at all that are in use; rf_cache_fork and rf_cache_drop
+ * copy numbers as they are): calls that write then change nothing, calls that read give arbitrary results for that sequence.
  */
 #define RF_CACHE_PAGE 128
 typedef struct {

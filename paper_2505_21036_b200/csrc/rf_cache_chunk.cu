@@ -13,11 +13,13 @@
 // the swizzled form that tcgen05 reads, beside the softmax.  A page's scale has to go into V or into the weights, as O adds up over pages:
 // V is held in units of 2^ref, ref the scale of the piece's first page, until a page's scale is more than 2^7 above it or 2^15 below, where fp16
 // would not hold it exactly: that page's scale is the next ref, and O is rescaled, as for a new maximum, in the rows that take
-// something of the page.  (Rare where a layer's pages are of like size.)  Only pages more than 2^60 below the largest unit so far lose places.  The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to
-// 2^-21 of the maximum and to 2^-31 of it in steps; a row of a million keys loses 2^-12 of its weight at most.
+// something of the page.  (Rare where a layer's pages are of like size.)  Only pages more than 2^60 below the largest unit so far lose places.
+// The weights are fp16 too: 2^7 at the running maximum, at most 2^15, exact to 11 bits down to 2^-21 of the maximum and to 2^-31 of it in
+// steps; a row of a million keys loses 2^-12 of its weight at most.
 // (V to bf16 in seven integer instructions and two products for four codes: 2050 cycles of the widening warps' 3470 a tile, beside the softmax
 // on the same integer pipes; 24 heads, 2040 rows, 32 896 keys, D = 128: 784 us, to fp16 764 (1070 TFLOP/s), with the widening left out 686.  K
-// widened as well, by the same four warps: 1090.  Repeated for a second the board's power limits it: 867.)
+// widened as well, by the same four warps: 1090.  Repeated for a second the board's power limits it: 870
+// to 896, by box.  The units that follow the pages cost 0.5 % of that, and 2 % where rows are ragged and lse is wanted.)
 // Warp roles:
 //   warps 0-3, 4-7   softmax of streams 0 and 1 (one thread per query row)
 //   warp 8           pages: walks the item's tiles, looks their pages and scales up (eight at a time), fetches Q and the codes by TMA
